@@ -524,6 +524,57 @@ grace_status_t grace_embed_bf16(const int32_t* token, const uint16_t* embed, con
 /* In place: logits fp32 [R][V] -> log-probabilities (natural log), normalised over all V. */
 grace_status_t grace_log_softmax(float* logits, int R, int V, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Decoder blocks with root-mean-square norms, products in 8 bits, biases and smooth activations (extensions: Section 3.2
+ * fixes neither normalisation nor feed-forward; SID generators of the T5 kind have the norm, others the biases).
+ * An e4m3 value is the 8-bit float with 4 exponent and 3 mantissa bits (largest 448, no infinity), passed as uint8_t.
+ * ---------------------------------------------------------------------------------------- */
+
+/* The residual stream takes a block's output and is normalised:
+ *   s = x + delta, rounded to x's type, kept in x_out;   n = s / sqrt(mean(s^2) + eps) * gamma
+ *   y_bf16: n;   y_e4m3 with y_scale: y_scale[r] = max(max|n[r]|, 2^-100) / 448 and y = n / y_scale[r]
+ * Exactly one of x_f32 / x_bf16 and exactly one of y_bf16 / y_e4m3 (then y_scale fp32 [R], else NULL).  delta (bf16) and
+ * x_out (x's type) are both given or both NULL (s = x, nothing kept); x_out may be x, with its row stride.  Otherwise
+ * outputs overlap nothing.  Row r of a tensor starts at r * its row stride (elements, >= D).  The norm is that of the
+ * stored stream: one call with delta gives the bits of an addition followed by a call without.
+ * Statistics in fp32.  A NaN stays in its row, whose y_scale is then NaN.  1 <= D <= 16384, any alignment of the
+ * elements' own; rows that all start on 16 bytes (y_e4m3: 8) with D % 8 == 0 take the wide form. */
+grace_status_t grace_rms_norm(const float* x_f32, const uint16_t* x_bf16, int64_t ldx, const uint16_t* delta,
+                              int64_t ld_delta, void* x_out, int64_t ldx_out, const float* gamma,
+                              uint16_t* y_bf16, uint8_t* y_e4m3, int64_t ldy, float* y_scale,
+                              int R, int D, float eps, void* stream);
+
+/* Host: rows of finite fp32 weights w [N][K] as e4m3 with one scale each, w_scale[n] = max(max|w[n]|, 2^-100) / 448 and
+ * w_e4m3 = w / w_scale[n] (nearest, ties to even): the operand w of grace_linear_act_e4m3. */
+grace_status_t grace_quantize_rows_e4m3(const float* w, int64_t N, int64_t K, uint8_t* w_e4m3, float* w_scale);
+
+/* ------------------------------------------------------------------------------------------
+ * Sampling in place of the ranking (an extension: Section 3.3 ranks): from every row, `draws` tokens with replacement, by
+ * given numbers u.  Row r = b * M + m; its candidates are the tokens whose bit is set in allow_bits (NULL: all V) and whose
+ * logit is not -inf, in the order (logit descending, token ascending; -0.0 == +0.0).  With w = e^((logit - max) / T):
+ *   top_k[b] > 0   only the first top_k candidates
+ *   top_p[b] < 1   of these the fewest, from the first on, whose w reach top_p of the sum of their w (at least one)
+ *   min_p[b] > 0   of these those with w >= min_p (the first always)
+ * Draw d takes the first kept token in ascending order at which the running sum of kept w exceeds u[r][d] times the whole.
+ * T = temperature[b]; T <= 0 or NaN: the first candidate.  Each of the four device arrays [B] may be NULL (T = 1, no limit).
+ *   logits      : fp32 or bf16 (exactly one), [B*M][V], row stride ld >= V; log-probabilities do as well
+ *   allow_bits  : uint64 [B*M][ceil(V/64)] as grace_gtm_mask* / grace_gtm_allow_bits leave them; logits of other tokens
+ *                 have no influence whatever they hold
+ *   row_score, row_lse : fp32 [B*M], as for grace_beam_topk_masked; NULL = 0
+ *   u           : fp32 [B*M][draws] in [0, 1)
+ * Outputs [B][M*draws], entry m*draws + d of request b: out_score = row_score + (logit - row_lse), out_logq = logarithm of
+ * the share of the kept w that the token has (the probability of this draw; may be NULL), out_parent = m (may be NULL),
+ * out_token: what grace_beam_update takes with K = M*draws.  A row without candidates: score and logq -inf, token 0.
+ * A NaN among a row's allowed logits sets GRACE_DEV_NAN and leaves the row without candidates.  Logits of +inf weigh
+ * 1 each and all others nothing.
+ * The tokens are those of this definition in 64-bit arithmetic.  Nothing depends on the order of the GPU's threads.
+ * V <= 65536, B*M < 2^31. */
+grace_status_t grace_sample(const float* logits_f32, const uint16_t* logits_bf16, int64_t ld, const uint64_t* allow_bits,
+                            const float* row_score, const float* row_lse, const float* temperature,
+                            const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+                            int B, int M, int V, int draws, float* out_score, float* out_logq,
+                            int32_t* out_parent, int32_t* out_token, int32_t* d_status, void* stream);
+
 /* Per-layer weights; every matrix is bf16 [out_features][in_features], dense rows. */
 typedef struct {
   const float *ln1_g, *ln1_b, *ln2_g, *ln2_b, *ln3_g, *ln3_b;

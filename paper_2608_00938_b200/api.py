@@ -142,6 +142,10 @@ _beam_update = _sig("grace_beam_update", _i32, [_vp, _vp, _vp, _vp, _vp, C.POINT
 _linear = _sig("grace_linear", _i32, [_vp, _i64, _vp, _i64, _vp, _vp, _i64, _vp, _i32, _i32, _i32, _i32, _vp])
 _linear_multi = _sig("grace_linear_multi", _i32, [_vp, _i64, _i32, C.POINTER(_vp), _i64, C.POINTER(_vp), _i64, _i32, _i32, _i32, _vp])
 _linear_add_bf16 = _sig("grace_linear_add_bf16", _i32, [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp])
+_rms_norm = _sig("grace_rms_norm", _i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i32, _i32, _f32, _vp])
+_quantize_rows_e4m3 = _sig("grace_quantize_rows_e4m3", _i32, [_vp, _i64, _i64, _vp, _vp])
+_sample = _sig("grace_sample", _i32, [_vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32,
+                                     _vp, _vp, _vp, _vp, _vp, _vp])
 _layer_norm_bf16 = _sig("grace_layer_norm_bf16", _i32, [_vp, _vp, _vp, _vp, _i32, _i32, _f32, _vp])
 _embed_bf16 = _sig("grace_embed_bf16", _i32, [_vp, _vp, _vp, _vp, _i32, _i32, _i32, _vp, _vp])
 _layer_norm = _sig("grace_layer_norm", _i32, [_vp, _vp, _vp, _vp, _i32, _i32, _f32, _vp])
@@ -180,6 +184,25 @@ def _hp(a, dtype):
 def _stream():
     import torch
     return torch.cuda.current_stream().cuda_stream
+
+
+def _need(ok, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _arg(t, where: str, name: str, dtype, shape=None, rows: bool = False):
+    """Device pointer of an optional tensor argument of the current device, checked: its type, its shape, and that it is
+    contiguous (rows: 2-D with contiguous rows)."""
+    import torch
+    if t is None:
+        return None
+    _need(t.is_cuda and t.get_device() == torch.cuda.current_device(), f"{where}: {name} is not on the current CUDA device")
+    _need(t.dtype == dtype, f"{where}: {name} is {t.dtype}, not {dtype}")
+    _need(shape is None or tuple(t.shape) == shape, f"{where}: {name} has shape {tuple(t.shape)}, not {shape}")
+    _need((t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)) if rows else t.is_contiguous(),
+          f"{where}: {name} {'has no contiguous rows' if rows else 'is not contiguous'}")
+    return t.data_ptr()
 
 
 def version() -> int:
@@ -634,6 +657,71 @@ def grace_layer_norm(x, gamma, beta, out, eps: float = 1e-5):
         return out
     _check(_layer_norm(_dp(x), _dp(gamma), _dp(beta), _dp(out), R, D, eps, _stream()), "grace_layer_norm")
     return out
+
+
+def _row_stride(t):
+    """Elements between rows; a single row may carry any stride, so it counts as its width."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
+
+
+def grace_quantize_rows_e4m3(w: np.ndarray):
+    """Host: fp32 [N, K] -> (e4m3 bit patterns uint8 [N, K], scales fp32 [N]): the weights of grace_linear_act."""
+    w = np.ascontiguousarray(w, dtype=np.float32)
+    _need(w.ndim == 2, "grace_quantize_rows_e4m3: w is not 2-D")
+    q, scale = np.empty(w.shape, np.uint8), np.empty(w.shape[0], np.float32)
+    _check(_quantize_rows_e4m3(w.ctypes.data, w.shape[0], w.shape[1], q.ctypes.data, scale.ctypes.data),
+           "grace_quantize_rows_e4m3")
+    return q, scale
+
+
+def grace_rms_norm(x, gamma, out, eps: float = 1e-6, delta=None, x_out=None, scale=None):
+    """out = s * rsqrt(mean(s^2) + eps) * gamma with s = x + delta, which x_out keeps (default: x, in place).
+
+    x fp32 or bf16 [R, D]; delta bf16 [R, D] or None; x_out as x; out bf16, or float8_e4m3fn with scale fp32 [R] (one scale
+    per row: the operand of grace_linear_act).  Rows may have any stride."""
+    import torch
+    where = "grace_rms_norm"
+    _need(x.dim() == 2 and x.dtype in (torch.float32, torch.bfloat16), f"{where}: x is not fp32 or bf16 [R, D]")
+    shape = R, D = tuple(x.shape)
+    f32, e4m3 = x.dtype == torch.float32, out.dtype == torch.float8_e4m3fn
+    xp = _arg(x, where, "x", x.dtype, shape, True)
+    if delta is None:
+        _need(x_out is None, f"{where}: x_out without delta")
+    elif x_out is None:
+        x_out = x
+    _need((scale is not None) == e4m3, f"{where}: scale belongs to an e4m3 out")
+    yp = _arg(out, where, "out", torch.float8_e4m3fn if e4m3 else torch.bfloat16, shape, True)
+    _check(_rms_norm(xp if f32 else None, None if f32 else xp, _row_stride(x), _arg(delta, where, "delta", torch.bfloat16, shape, True),
+                     0 if delta is None else _row_stride(delta), _arg(x_out, where, "x_out", x.dtype, shape, True),
+                     0 if x_out is None else _row_stride(x_out), _arg(gamma, where, "gamma", torch.float32, (D,)),
+                     None if e4m3 else yp, yp if e4m3 else None, _row_stride(out),
+                     _arg(scale, where, "scale", torch.float32, (R,)), R, D, eps, _stream()), where)
+    return out
+
+
+def grace_sample(logits, u, out_score, out_token, B: int, M: int, allow_bits=None, row_score=None, row_lse=None, temperature=None,
+                 top_k=None, top_p=None, min_p=None, out_logq=None, out_parent=None, d_status=None):
+    """Draws u.shape[1] tokens from every row of logits fp32 or bf16 [B*M, V] (any row stride) by the numbers u fp32 [B*M, draws].
+
+    allow_bits int64 [B*M, ceil(V/64)]; row_score, row_lse fp32 [B*M]; temperature, top_p, min_p fp32 [B], top_k int32 [B] (None: 1
+    and no limit).  Outputs of B*M*draws elements each: out_score, out_logq fp32, out_token, out_parent int32."""
+    import torch
+    where = "grace_sample"
+    _need(logits.dim() == 2 and logits.dtype in (torch.float32, torch.bfloat16), f"{where}: logits are not fp32 or bf16 [R, V]")
+    R, V = logits.shape
+    _need(R == B * M and u.dim() == 2, f"{where}: logits have {R} rows, not {B} x {M}, or u is not 2-D")
+    draws = u.shape[1]
+    f32, i32, bf16 = torch.float32, torch.int32, logits.dtype == torch.bfloat16
+    lp = _arg(logits, where, "logits", logits.dtype, None, True)
+    for name, t in (("out_score", out_score), ("out_token", out_token), ("out_logq", out_logq), ("out_parent", out_parent)):
+        _need(t is None or t.numel() == R * draws, f"{where}: {name} does not hold {R} x {draws} elements")
+    _check(_sample(None if bf16 else lp, lp if bf16 else None, _row_stride(logits),
+                   _arg(allow_bits, where, "allow_bits", torch.int64, (R, (V + 63) // 64)), _arg(row_score, where, "row_score", f32, (R,)),
+                   _arg(row_lse, where, "row_lse", f32, (R,)), _arg(temperature, where, "temperature", f32, (B,)),
+                   _arg(top_k, where, "top_k", i32, (B,)), _arg(top_p, where, "top_p", f32, (B,)), _arg(min_p, where, "min_p", f32, (B,)),
+                   _arg(u, where, "u", f32, (R, draws)), B, M, V, draws, _arg(out_score, where, "out_score", f32),
+                   _arg(out_logq, where, "out_logq", f32), _arg(out_parent, where, "out_parent", i32), _arg(out_token, where, "out_token", i32),
+                   _arg(d_status, where, "d_status", i32), _stream()), where)
 
 
 def grace_embed(token, embed, pos, x, d_status=None):

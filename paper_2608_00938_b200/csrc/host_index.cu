@@ -4,8 +4,10 @@
 #include <string>
 #include <unordered_map>
 #include <algorithm>
+#include <cmath>
 #include <vector>
 
+#include <cuda_fp8.h>
 #include "common.cuh"
 
 namespace {
@@ -413,6 +415,22 @@ inline float bf16_to_f32(uint16_t b) {
 extern "C" grace_status_t grace_f32_to_bf16(const float* a, int64_t n, uint16_t* out) {
   if (!a || !out || n < 0) return GRACE_INVALID_ARG;
   for (int64_t i = 0; i < n; ++i) out[i] = f32_to_bf16_rne(a[i]);
+  return GRACE_OK;
+}
+
+extern "C" grace_status_t grace_quantize_rows_e4m3(const float* w, int64_t N, int64_t K, uint8_t* w_e4m3, float* w_scale) {
+  if (!w || !w_e4m3 || !w_scale || N <= 0 || K <= 0) return GRACE_INVALID_ARG;
+  for (int64_t n = 0; n < N; ++n) {
+    const float* row = w + n * K;
+    float most = 0x1p-100f;
+    for (int64_t k = 0; k < K; ++k) {
+      if (!std::isfinite(row[k])) return GRACE_INVALID_ARG;
+      most = std::max(most, std::fabs(row[k]));
+    }
+    const float scale = most / 448.f;
+    w_scale[n] = scale;
+    for (int64_t k = 0; k < K; ++k) w_e4m3[n * K + k] = __nv_cvt_float_to_fp8(row[k] / scale, __NV_SATFINITE, __NV_E4M3);
+  }
   return GRACE_OK;
 }
 
