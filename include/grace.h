@@ -548,6 +548,28 @@ grace_status_t grace_rms_norm(const float* x_f32, const uint16_t* x_bf16, int64_
  * w_e4m3 = w / w_scale[n] (nearest, ties to even): the operand w of grace_linear_act_e4m3. */
 grace_status_t grace_quantize_rows_e4m3(const float* w, int64_t N, int64_t K, uint8_t* w_e4m3, float* w_scale);
 
+typedef enum {
+  GRACE_ACT_NONE = 0,
+  GRACE_ACT_RELU = 1,
+  GRACE_ACT_GELU = 2,           /* v Phi(v), Phi the normal distribution function             */
+  GRACE_ACT_GELU_TANH = 3,      /* v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2             */
+  GRACE_ACT_SILU = 4            /* v / (1 + e^-v)                                              */
+} grace_act_t;
+
+/* y = act(x @ w^T + bias) + residual: grace_linear with a bias, the activations above and a residual of y's type behind
+ * them.  x bf16 [M][K] (row stride ldx), w bf16 [N][K] (ldw), bias fp32 [N] or NULL; exactly one of y_bf16 / y_f32 ([M][N],
+ * row stride ldy); residual: same type as y, [M][N], row stride ldr, or NULL; it may be y itself (ldr = ldy), otherwise y
+ * overlaps nothing.  fp32 accumulation, one rounding of the result.  x and w 16-byte aligned with row strides that are
+ * multiples of 8 elements, K a multiple of 8; M, N, and the alignment of y, residual and bias (their elements' own) are free. */
+grace_status_t grace_linear_act(const uint16_t* x, int64_t ldx, const uint16_t* w, int64_t ldw, const float* bias, int act,
+                                const void* residual, int64_t ldr, uint16_t* y_bf16, float* y_f32, int64_t ldy,
+                                int M, int N, int K, void* stream);
+/* The same with e4m3 operands: y = act(x_scale[m] w_scale[n] (x @ w^T) + bias) + residual.  x_scale fp32 [M] and w_scale
+ * fp32 [N], as grace_rms_norm and grace_quantize_rows_e4m3 give them; NULL: 1.  Row strides of x and w and K: multiples of 16. */
+grace_status_t grace_linear_act_e4m3(const uint8_t* x, int64_t ldx, const float* x_scale, const uint8_t* w, int64_t ldw,
+                                     const float* w_scale, const float* bias, int act, const void* residual, int64_t ldr,
+                                     uint16_t* y_bf16, float* y_f32, int64_t ldy, int M, int N, int K, void* stream);
+
 /* ------------------------------------------------------------------------------------------
  * Sampling in place of the ranking (an extension: Section 3.3 ranks): from every row, `draws` tokens with replacement, by
  * given numbers u.  Row r = b * M + m; its candidates are the tokens whose bit is set in allow_bits (NULL: all V) and whose

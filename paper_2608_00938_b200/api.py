@@ -24,6 +24,7 @@ lib = C.CDLL(LIB_PATH)
 GRACE_OK = 0
 DEV_BAD_INDEX, DEV_NAN, DEV_TIMEOUT, DEV_TOPK_EXACT_PATH = 1, 2, 4, 8
 MATCH_NONE, MATCH_NODE_BITMASK, MATCH_PREFIX_BLOOM = 0, 1, 2
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 MAX_LAYERS, MAX_STEPS = 16, 8
 
 _vp, _i32, _i64, _f32, _sz = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_size_t
@@ -144,6 +145,9 @@ _linear_multi = _sig("grace_linear_multi", _i32, [_vp, _i64, _i32, C.POINTER(_vp
 _linear_add_bf16 = _sig("grace_linear_add_bf16", _i32, [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32, _vp])
 _rms_norm = _sig("grace_rms_norm", _i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _i64, _vp, _i32, _i32, _f32, _vp])
 _quantize_rows_e4m3 = _sig("grace_quantize_rows_e4m3", _i32, [_vp, _i64, _i64, _vp, _vp])
+_linear_act = _sig("grace_linear_act", _i32, [_vp, _i64, _vp, _i64, _vp, _i32, _vp, _i64, _vp, _vp, _i64, _i32, _i32, _i32, _vp])
+_linear_act_e4m3 = _sig("grace_linear_act_e4m3", _i32, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _i32, _vp, _i64, _vp, _vp, _i64,
+                                                       _i32, _i32, _i32, _vp])
 _sample = _sig("grace_sample", _i32, [_vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32,
                                      _vp, _vp, _vp, _vp, _vp, _vp])
 _layer_norm_bf16 = _sig("grace_layer_norm_bf16", _i32, [_vp, _vp, _vp, _vp, _i32, _i32, _f32, _vp])
@@ -697,6 +701,32 @@ def grace_rms_norm(x, gamma, out, eps: float = 1e-6, delta=None, x_out=None, sca
                      None if e4m3 else yp, yp if e4m3 else None, _row_stride(out),
                      _arg(scale, where, "scale", torch.float32, (R,)), R, D, eps, _stream()), where)
     return out
+
+
+def grace_linear_act(x, w, y, bias=None, act: str = "none", residual=None, x_scale=None, w_scale=None):
+    """y = act(x_scale[:, None] * w_scale * (x @ w.T) + bias) + residual.
+
+    x [M, K], w [N, K]: both bf16 (no scales) or both float8_e4m3fn with x_scale fp32 [M], w_scale fp32 [N] (None: 1); bias fp32 [N];
+    y [M, N] bf16 or fp32; residual as y (may be y).  act: none, relu, gelu, gelu_tanh, silu.  Rows may have any stride."""
+    import torch
+    where = "grace_linear_act"
+    _need(act in ACTIVATIONS, f"{where}: no activation {act!r}")
+    _need(x.dim() == 2 and w.dim() == 2 and x.shape[1] == w.shape[1], f"{where}: x {tuple(x.shape)} and w {tuple(w.shape)} do not multiply")
+    (M, K), N = x.shape, w.shape[0]
+    f32, e4m3 = y.dtype == torch.float32, x.dtype == torch.float8_e4m3fn
+    kind = torch.float8_e4m3fn if e4m3 else torch.bfloat16
+    _need(e4m3 or (x_scale is None and w_scale is None), f"{where}: scales belong to e4m3 operands")
+    xp, wp = _arg(x, where, "x", kind, None, True), _arg(w, where, "w", kind, None, True)
+    yp = _arg(y, where, "y", torch.float32 if f32 else torch.bfloat16, (M, N), True)
+    rp, ldr = _arg(residual, where, "residual", y.dtype, (M, N), True), 0 if residual is None else _row_stride(residual)
+    rest = (_arg(bias, where, "bias", torch.float32, (N,)), ACTIVATIONS[act], rp, ldr, None if f32 else yp, yp if f32 else None, _row_stride(y),
+            M, N, K, _stream())
+    if e4m3:
+        _check(_linear_act_e4m3(xp, _row_stride(x), _arg(x_scale, where, "x_scale", torch.float32, (M,)), wp, _row_stride(w),
+                                _arg(w_scale, where, "w_scale", torch.float32, (N,)), *rest), where)
+    else:
+        _check(_linear_act(xp, _row_stride(x), wp, _row_stride(w), *rest), where)
+    return y
 
 
 def grace_sample(logits, u, out_score, out_token, B: int, M: int, allow_bits=None, row_score=None, row_lse=None, temperature=None,

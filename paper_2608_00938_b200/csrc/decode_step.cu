@@ -222,11 +222,13 @@ namespace grace {
 int linear_tc_timeouts();
 int cross_attn_tc_timeouts();
 int layer_chain_timeouts();
+int linear_act_tc_timeouts();
 }  // namespace grace
 
 extern "C" int grace_wait_timeouts(void) {
   const int a = grace::linear_tc_timeouts(), b = grace::cross_attn_tc_timeouts(), c = grace::layer_chain_timeouts();
-  return (a < 0 || b < 0 || c < 0) ? -1 : a + b + c;
+  const int d = grace::linear_act_tc_timeouts();
+  return (a < 0 || b < 0 || c < 0 || d < 0) ? -1 : a + b + c + d;
 }
 
 // Keeps part of a buffer that many kernels of a step re-read (the residual stream: three add-reductions,
