@@ -19,20 +19,89 @@ struct ActParams {
   int M, N, KB, act;                                       // KB: k-blocks (the last one filled up with zeros)
 };
 
-// All activations but ReLU in the form v times a factor of (0, 1).
-__device__ __forceinline__ float act_of(float v, int act) {
+__device__ __forceinline__ float act_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float act_rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// An epilogue's activations are bound by the MUFU pipe (an exponential or a reciprocal is 8 clocks of a scheduler's, a
+// packed fma of two elements one slot), so a pair of elements takes two exponentials and at most one reciprocal:
+//   v / (1 + 2^s), v' / (1 + 2^s'): with a = 1 + 2^s, b = 1 + 2^s', r = 1 / (a b):  v b r and v' a r.
+// s is held at 60 (2^120 and its reciprocal are fp32 numbers): below, the results are smaller than 2^-54.
+// (Scalar operations: a packed one of two elements saves a slot, but takes its constants from register pairs, which cost two
+// more to fill where registers are short.)
+__device__ __forceinline__ void act_over_pair(float& v0, float& v1, float s0, float s1) {
+  const float a = act_ex2(fminf(s0, 60.f)) + 1.f, b = act_ex2(fminf(s1, 60.f)) + 1.f;
+  const float r = act_rcp(a * b);
+  v0 *= b * r;
+  v1 *= a * r;
+}
+__device__ __forceinline__ void act_silu(float& v0, float& v1) {
+  constexpr float kLog2e = 1.4426950408889634f;
+  act_over_pair(v0, v1, -kLog2e * v0, -kLog2e * v1);
+}
+__device__ __forceinline__ void act_gelu_tanh(float& v0, float& v1) {
+  // (1 + tanh z) / 2 = 1 / (1 + e^-2z), 2z = sqrt(8 / pi) (v + 0.044715 v^3), times log2(e)
+  act_over_pair(v0, v1, v0 * fmaf(v0 * v0, -0.10294324f, -2.3022082f), v1 * fmaf(v1 * v1, -0.10294324f, -2.3022082f));
+}
+// v Phi(v) = max(v, 0) - a Phi(-a), a = |v|, and Phi(-a) = 2^P(a) with P of degree 5: log2 Phi(-a) is smooth and nearly
+// quadratic.  P is a minimax fit of it on [0, 5] (weighted least squares, reweighted by the error): Phi(-a) is within 7.5e-5 of
+// itself, 1 / 26 of half a bf16 step, and P goes on falling behind.  For bf16 results; fp32 ones take erff.
+__device__ __forceinline__ float act_gelu_one(float v) {
+  const float a = fminf(fabsf(v), 16.f);
+  float q = fmaf(a, -3.292835899628699e-4f, 5.912758409976959e-3f);
+  q = fmaf(a, q, -4.852477088570595e-2f);
+  q = fmaf(a, q, -4.6373286843299866e-1f);
+  q = fmaf(a, q, -1.149355173110962f);
+  q = fmaf(a, q, -1.000108003616333f);
+  return fmaf(-a, act_ex2(q), fmaxf(v, 0.f));
+}
+__device__ __forceinline__ void act_gelu_bf16(float& v0, float& v1) { v0 = act_gelu_one(v0); v1 = act_gelu_one(v1); }
+__device__ __forceinline__ void act_gelu_f32(float& v0, float& v1) {
+  v0 = 0.5f * v0 * (1.f + erff(v0 * 0.70710678118654752f));
+  v1 = 0.5f * v1 * (1.f + erff(v1 * 0.70710678118654752f));
+}
+// The activation of a whole array: one branch for all of it (one per element is an indirect branch each: 65536 x 2048 x 512
+// took 463 us so, without any activation).
+template <bool F32, int N>
+__device__ __forceinline__ void act_all(float (&v)[N], int act) {
+  auto all = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) f(v[i], v[i + 1]);
+  };
   switch (act) {
-    case GRACE_ACT_RELU: return fmaxf(v, 0.f);
-    case GRACE_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
-    case GRACE_ACT_GELU_TANH: {
-      const float t = v * fmaf(0.0713548162726f, v * v, 1.59576912160573f);      // 2 sqrt(2/pi) (v + 0.044715 v^3)
-      return __fdividef(v, 1.f + __expf(-t));
-    }
-    case GRACE_ACT_SILU: return __fdividef(v, 1.f + __expf(-v));
-    default: return v;
+    case GRACE_ACT_RELU: all([](float& x, float& y) { x = fmaxf(x, 0.f); y = fmaxf(y, 0.f); }); break;
+    case GRACE_ACT_GELU: if constexpr (F32) all(act_gelu_f32); else all(act_gelu_bf16); break;
+    case GRACE_ACT_GELU_TANH: all(act_gelu_tanh); break;
+    case GRACE_ACT_SILU: all(act_silu); break;
   }
 }
 
+// v = acc * xs * scale + bias of 32 columns, whose scales and biases (64 floats behind the scales) lie in shared memory.
+template <bool F8>
+__device__ __forceinline__ void act_affine(float (&v)[32], const uint32_t (&acc)[32], float xs, const float* scale) {
+  const f32x2_t x2 = f2_pack(xs, xs);
+#pragma unroll
+  for (int i = 0; i < 32; i += 4) {
+    const float4 b4 = *reinterpret_cast<const float4*>(scale + 64 + i);
+    f32x2_t lo = f2_pack(__uint_as_float(acc[i]), __uint_as_float(acc[i + 1])), hi = f2_pack(__uint_as_float(acc[i + 2]), __uint_as_float(acc[i + 3]));
+    if (F8) {
+      const float4 s4 = *reinterpret_cast<const float4*>(scale + i);
+      lo = f2_fma(f2_mul(lo, x2), f2_pack(s4.x, s4.y), f2_pack(b4.x, b4.y));
+      hi = f2_fma(f2_mul(hi, x2), f2_pack(s4.z, s4.w), f2_pack(b4.z, b4.w));
+    } else {
+      lo = f2_add(lo, f2_pack(b4.x, b4.y));
+      hi = f2_add(hi, f2_pack(b4.z, b4.w));
+    }
+    f2_unpack(lo, v[i], v[i + 1]);
+    f2_unpack(hi, v[i + 2], v[i + 3]);
+  }
+}
 template <bool F8, bool PAIR>
 __device__ __forceinline__ void act_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   if (PAIR) {
@@ -218,9 +287,10 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
       for (int j = 0; j < 16; j += 4) {
         const float4 ws = *reinterpret_cast<const float4*>(col_s + c + j);
         const float4 bb = *reinterpret_cast<const float4*>(col_s + kSlice + c + j);
-        v[j] = act_of(fmaf(v[j] * xs, ws.x, bb.x), p.act); v[j + 1] = act_of(fmaf(v[j + 1] * xs, ws.y, bb.y), p.act);
-        v[j + 2] = act_of(fmaf(v[j + 2] * xs, ws.z, bb.z), p.act); v[j + 3] = act_of(fmaf(v[j + 3] * xs, ws.w, bb.w), p.act);
+        v[j] = fmaf(v[j] * xs, ws.x, bb.x); v[j + 1] = fmaf(v[j + 1] * xs, ws.y, bb.y);
+        v[j + 2] = fmaf(v[j + 2] * xs, ws.z, bb.z); v[j + 3] = fmaf(v[j + 3] * xs, ws.w, bb.w);
       }
+      act_all<F32>(v, p.act);
       if (p.residual != nullptr) {
         if (whole && wide_r) {
 #pragma unroll
@@ -271,38 +341,41 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 
 // ---------------------------------------------------------------------------------------------
 // Persistent CTA pairs: 256 x 256 tiles (n fastest), each CTA with 128 rows of x and 128 of the tile's rows of w in a ring of
-// five stages, one tcgen05.mma stream per pair into one of two accumulators (all of TMEM).  Eight epilogue warps per CTA in
-// two groups of four, each with 128 of the tile's columns and two staging buffers of 128 rows x 128 bytes: the residual comes
-// into a buffer by TMA, the group adds it where it lies and hands the buffer to a TMA store, so that neither passes through
-// strided accesses.  (Eight warps and not four: an e4m3 product of K = 512 has 2048 clocks of MMAs per tile, and a smooth
-// activation takes an exponential and a quotient for each of 128 x 256 elements of a CTA.)
+// five stages, one tcgen05.mma stream per pair into one of two accumulators (all of TMEM).
+// Epilogue: sixteen warps per CTA, each with 32 rows x 64 columns of its own.  A thread has a row: it takes 32 columns at a
+// time out of the accumulator, finishes them and leaves them in the warp's 4 KB of shared memory (128 bytes a row, swizzled),
+// from where a TMA store takes them.  The residual comes the same way: whole row segments into registers while the warp waits
+// for the accumulator, from there into the 4 KB, and a thread adds its row's where the results will lie.  No warp waits for
+// another.  WIDE: rows of y and of the residual start on 16 bytes; otherwise
+// the warp moves single elements between the 4 KB and memory.
+// (Eight warps in two groups that share a buffer and its barriers: 84 us for 65536 x 2048 x 512 in e4m3, without activation.)
 // ---------------------------------------------------------------------------------------------
-constexpr int kAPStages = 5;
+constexpr int kAPStages = 4;
 constexpr int kAPStageBytes = 2 * 128 * 128;
-constexpr int kAPStaging = 128 * 128;
-constexpr int kAPSmem = kAPStages * kAPStageBytes + 4 * kAPStaging + 256 + 2 * 256 * 4;
-constexpr int kAPThreads = 320;
+constexpr int kAPWarps = 16;
+constexpr int kAPTurn = 32 * 128;                          // 32 rows of 64 bf16 or 32 fp32
+constexpr int kAPCols = 2 * 64 * 4;                         // scales and biases of the warp's 64 columns
+constexpr int kAPSmem = kAPStages * kAPStageBytes + kAPWarps * (kAPTurn + kAPCols) + 256;
+constexpr int kAPThreads = 64 + 32 * kAPWarps;
 static_assert(kAPSmem >= tc::kTmemAllSmem && kAPSmem <= 227 * 1024, "");
 
-template <bool F8, bool F32>
+template <bool F8, bool F32, bool WIDE>
 __global__ void __launch_bounds__(kAPThreads, 1)
 act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
-                const __grid_constant__ CUtensorMap map_y, const __grid_constant__ CUtensorMap map_r, const ActParams p) {
+                const __grid_constant__ CUtensorMap map_y, const ActParams p) {
   extern __shared__ __align__(1024) uint8_t smem_pair[];
   uint8_t* tiles = smem_pair;
   if ((tc::smem_addr(tiles) & 1023u) != 0) {               // the swizzled tiles need it; same answer in every thread
     if (threadIdx.x == 0 && blockIdx.x == 0) atomicAdd(&tc::g_tc_timeouts, 1);
     return;
   }
-  uint8_t* staging = tiles + kAPStages * kAPStageBytes;    // [2 groups][2]
-  uint64_t* full = reinterpret_cast<uint64_t*>(staging + 4 * kAPStaging);       // even CTA only: both CTAs' bytes landed
+  uint8_t* turns = tiles + kAPStages * kAPStageBytes;
+  uint64_t* full = reinterpret_cast<uint64_t*>(turns + kAPWarps * (kAPTurn + kAPCols));  // even CTA only: both CTAs' bytes landed
   uint64_t* empty = full + kAPStages;                      // the pair's MMAs have read the stage
   uint64_t* acc_full = empty + kAPStages;                  // [2]
-  uint64_t* acc_empty = acc_full + 2;                      // [2] even CTA only: 8 local + 8 remote epilogue warps
-  uint64_t* res_full = acc_empty + 2;                      // [2 groups][2]
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(res_full + 4);
+  uint64_t* acc_empty = acc_full + 2;                      // [2] even CTA only: the epilogue warps of both
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  float* col_s = reinterpret_cast<float*>(staging + 4 * kAPStaging + 256);      // [256] scales, [256] biases
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_cta_rank();            // 0: issues the MMAs; 1: peer
@@ -312,11 +385,11 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kAPStages; ++s) { tc::mbar_init(full + s, 1); tc::mbar_init(empty + s, 1); }
-    for (int a = 0; a < 2; ++a) { tc::mbar_init(acc_full + a, 1); tc::mbar_init(acc_empty + a, 16); }
-    for (int a = 0; a < 4; ++a) tc::mbar_init(res_full + a, 1);
+    for (int a = 0; a < 2; ++a) { tc::mbar_init(acc_full + a, 1); tc::mbar_init(acc_empty + a, 2 * kAPWarps); }
     *abort_flag = 0;
     tc::fence_mbar_init();
-    tc::tma_prefetch_desc(&map_x); tc::tma_prefetch_desc(&map_w); tc::tma_prefetch_desc(&map_y);
+    tc::tma_prefetch_desc(&map_x); tc::tma_prefetch_desc(&map_w);
+    if (WIDE) tc::tma_prefetch_desc(&map_y);
   }
   if (warp == 0) tc::tmem_alloc_pair(tmem_slot, 512);
   tc::tc_fence_before();
@@ -370,61 +443,100 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       }
     }
   } else {
-    // ---- epilogue warps 2..9: group of 128 columns, TMEM lane quarter q = rows q*32 + lane of this CTA's 128 ----
-    const int group = (warp - 2) >> 2, q = warp & 3, row = q * 32 + lane;
-    const bool issuer = warp == 2 + 4 * group && lane == 0;
-    constexpr int kCols = F32 ? 32 : 64, kChunks = 128 / kCols;                  // columns of a staging buffer
-    uint8_t* const bufs = staging + group * 2 * kAPStaging;
-    const bool res = p.residual != nullptr;
-    int local = 0, g = 0;                                   // g: chunks of this group so far
-    // chunk g's residual into its buffer; the stores that used the buffer have been read out of it (bulk_wait_read)
-    auto fetch_residual = [&](int tile, int chunk, int at) {
-      if (tile >= total) return;
-      uint64_t* bar = res_full + 2 * group + (at & 1);
-      tc::mbar_expect_tx(bar, kAPStaging);
-      tc::tma_load_2d(bufs + (at & 1) * kAPStaging, &map_r, bar, (tile % n_tiles) * 256 + group * 128 + chunk * kCols,
-                      (tile / n_tiles) * 256 + (int)rank * 128);
-    };
-    float xs_next = 1.f, ws_next = 1.f, bias_next = 0.f;
-    auto fetch_vectors = [&](int tile) {                    // one tile ahead, from clamped addresses
-      tile = min(tile, total - 1);
-      const int m = min((tile / n_tiles) * 256 + (int)rank * 128 + row, p.M - 1), n = min((tile % n_tiles) * 256 + group * 128 + row, p.N - 1);
-      if (p.x_scale != nullptr) xs_next = __ldg(p.x_scale + m);
-      if (p.w_scale != nullptr) ws_next = __ldg(p.w_scale + n);
-      if (p.bias != nullptr) bias_next = __ldg(p.bias + n);
-    };
-    fetch_vectors(pair);
-    if (res && issuer) fetch_residual(pair, 0, 0);
-    for (int tile = pair; tile < total; tile += n_pairs, ++local) {
-      const int m0 = (tile / n_tiles) * 256 + (int)rank * 128, n0 = (tile % n_tiles) * 256 + group * 128;
-      const int ab = local & 1;
-      const float xs = xs_next;
-      // read behind the first chunk's barrier; the previous tile's readers are past its last one
-      col_s[group * 128 + row] = ws_next;
-      col_s[256 + group * 128 + row] = bias_next;
-      fetch_vectors(tile + n_pairs);
-      // a group goes on or stops as one, whatever a warp's own wait saw: the barriers below count on all four
-      if (!tc::named_bar_and(1 + group, 128, tc::mbar_wait_cluster(acc_full + ab, (local >> 1) & 1, abort_flag))) break;
-      tc::tc_fence_after();
-      const uint32_t t_acc = tmem_base + (uint32_t)(ab * 256 + group * 128) + ((uint32_t)(q * 32) << 16);
-#pragma unroll 1
-      for (int c = 0; c < kChunks; ++c, ++g) {
-        uint8_t* buf = bufs + (g & 1) * kAPStaging;
-        uint32_t r[kCols / 32][32];
+    // ---- epilogue warps 2..17: rows q*32 .. of this CTA's 128 (q: the warp's TMEM lane quarter), 64 columns ----
+    const int q = warp & 3, col = ((warp - 2) >> 2) * 64;
+    uint8_t* const turn = turns + (warp - 2) * kAPTurn;     // [32 rows][8 pieces of 16 bytes], swizzled by the row
+    uint4* const my_row = reinterpret_cast<uint4*>(turn + lane * 128);
+    constexpr int kSize = F32 ? 4 : 2, kPer = 16 / kSize, kCols = 128 / kSize;  // columns of a piece, of the 4 KB
+    auto element = [&](int row, int c) { return turn + row * 128 + (((c / kPer) ^ (row & 7)) << 4) + (c % kPer) * kSize; };
+    uint4 held[8];                                          // the residual of the next kCols columns
+    auto hold = [&](int m0, int n0) {
 #pragma unroll
-        for (int h = 0; h < kCols / 32; ++h) tc::tmem_ld32(t_acc + (uint32_t)(c * kCols + h * 32), r[h]);
-        if (issuer) {
-          if (res) {
-            tc::bulk_wait_read<0>();                       // the last store has been read out of the other buffer
-            if (c + 1 < kChunks) fetch_residual(tile, c + 1, g + 1); else fetch_residual(tile + n_pairs, 0, g + 1);
+      for (int i = 0; i < 8; ++i) {
+        const int m = m0 + 4 * i + (lane >> 3), n = n0 + (lane & 7) * kPer;
+        held[i] = make_uint4(0, 0, 0, 0);
+        if (WIDE && m < p.M && n < p.N) {                   // (not .nc: the residual may be y itself)
+          const char* at = reinterpret_cast<const char*>(p.residual) + ((int64_t)m * p.ldr + n) * kSize;
+          if (n + kPer <= p.N) {
+            held[i] = *reinterpret_cast<const uint4*>(at);
           } else {
-            tc::bulk_wait_read<1>();                       // the store that last used `buf` has been read out of it
+            uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+              if (n + e >= p.N) continue;
+              if (F32) w[e & 3] = reinterpret_cast<const uint32_t*>(at)[e];
+              else w[(e >> 1) & 3] |= (uint32_t)reinterpret_cast<const uint16_t*>(at)[e] << (16 * (e & 1));
+            }
+            held[i] = make_uint4(w[0], w[1], w[2], w[3]);
           }
         }
-        tc::named_bar_sync(1 + group, 128);
-        if (res) tc::mbar_wait(res_full + 2 * group + (g & 1), (g >> 1) & 1, abort_flag);   // (gives up: the tile is lost, as reported)
+      }
+    };
+    // the row's scale and the columns' vectors, one tile ahead; the latter in a copy of the warp's own
+    float* const scale = reinterpret_cast<float*>(turns + kAPWarps * kAPTurn + (warp - 2) * kAPCols);
+    float xs_next = 1.f, col_next[4] = {1.f, 1.f, 0.f, 0.f};
+    auto fetch = [&](int tile) {
+      tile = min(tile, total - 1);
+      const int m = min((tile / n_tiles) * 256 + (int)rank * 128 + q * 32 + lane, p.M - 1), n = (tile % n_tiles) * 256 + col + lane;
+      if (F8 && p.x_scale != nullptr) xs_next = __ldg(p.x_scale + m);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (F8 && p.w_scale != nullptr) col_next[i] = __ldg(p.w_scale + min(n + 32 * i, p.N - 1));
+        if (p.bias != nullptr) col_next[2 + i] = __ldg(p.bias + min(n + 32 * i, p.N - 1));
+      }
+    };
+    fetch(pair);
+    int local = 0;
+    for (int tile = pair; tile < total; tile += n_pairs, ++local) {
+      const int m0 = (tile / n_tiles) * 256 + (int)rank * 128 + q * 32, n0 = (tile % n_tiles) * 256 + col;
+      const int ab = local & 1;
+      if (WIDE && p.residual != nullptr) hold(m0, n0);
+      const float xs = xs_next;
+      __syncwarp();                                         // the tile in front has been finished with them
+#pragma unroll
+      for (int i = 0; i < 4; ++i) scale[32 * i + lane] = col_next[i];
+      fetch(tile + n_pairs);
+      bool ok = tc::mbar_wait_cluster(acc_full + ab, (local >> 1) & 1, abort_flag);
+      ok = __all_sync(kFullMask, ok);
+      if (!ok) break;
+      tc::tc_fence_after();
+      const uint32_t t_acc = tmem_base + (uint32_t)(ab * 256 + col) + ((uint32_t)(q * 32) << 16);
+      const bool in = m0 < p.M;
+#pragma unroll 1
+      for (int h = 0; h < 2; ++h) {
+        if (h * 32 % kCols == 0) {                          // a new filling of the 4 KB
+          if (WIDE) {
+            if (lane == 0) tc::bulk_wait_read<0>();
+            __syncwarp();
+            if (p.residual != nullptr) {
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                const int row = 4 * i + (lane >> 3);
+                *reinterpret_cast<uint4*>(turn + row * 128 + (((lane & 7) ^ (row & 7)) << 4)) = held[i];
+              }
+              if (kCols == 32 && h == 0) hold(m0, n0 + 32);
+              __syncwarp();
+            }
+          } else {
+            __syncwarp();
+            if (p.residual != nullptr && in) {
+#pragma unroll 4
+              for (int row = 0; row < 32; ++row) {
+                const char* at = reinterpret_cast<const char*>(p.residual) + ((int64_t)(m0 + row) * p.ldr + n0 + 32 * h) * kSize;
+                for (int c = lane; c < kCols; c += 32) {
+                  if (m0 + row >= p.M || n0 + 32 * h + c >= p.N) continue;
+                  if (F32) *reinterpret_cast<uint32_t*>(element(row, c)) = reinterpret_cast<const uint32_t*>(at)[c];
+                  else *reinterpret_cast<uint16_t*>(element(row, c)) = reinterpret_cast<const uint16_t*>(at)[c];
+                }
+              }
+              __syncwarp();
+            }
+          }
+        }
+        uint32_t r[32];
+        tc::tmem_ld32(t_acc + 32 * h, r);
         tc::tmem_ld_wait();
-        if (c == kChunks - 1) {                            // accumulator fully read: hand it back to the issuer
+        if (h == 1) {                                       // this part of the accumulator has been read
           tc::tc_fence_before();
           __syncwarp();
           if (lane == 0) {
@@ -432,45 +544,51 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             else tc::mbar_arrive_remote(acc_empty + ab, 0);
           }
         }
-        uint4* my_row = reinterpret_cast<uint4*>(buf + row * 128);
-        const float* ws = col_s + group * 128 + c * kCols;
-        const float* bb = ws + 256;
-        constexpr int kPiece = F32 ? 4 : 8;                // elements of 16 bytes
+        float v[32];
+        act_affine<F8>(v, r, xs, scale + 32 * h);
+        act_all<F32>(v, p.act);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float v[kPiece];
-#pragma unroll
-          for (int e = 0; e < kPiece; e += 4) {
-            const int i = kPiece * j + e;
-            const float4 s4 = *reinterpret_cast<const float4*>(ws + i), b4 = *reinterpret_cast<const float4*>(bb + i);
-            const uint32_t* a = &r[i >> 5][i & 31];
-            v[e] = act_of(fmaf(__uint_as_float(a[0]) * xs, s4.x, b4.x), p.act);
-            v[e + 1] = act_of(fmaf(__uint_as_float(a[1]) * xs, s4.y, b4.y), p.act);
-            v[e + 2] = act_of(fmaf(__uint_as_float(a[2]) * xs, s4.z, b4.z), p.act);
-            v[e + 3] = act_of(fmaf(__uint_as_float(a[3]) * xs, s4.w, b4.w), p.act);
-          }
-          uint4* at = my_row + (j ^ (row & 7));
-          if (res) {
+        for (int j = 0; j < 32 / kPer; ++j) {
+          uint4* at = my_row + (((h * 32 % kCols) / kPer + j) ^ (lane & 7));
+          float* e = v + kPer * j;
+          if (p.residual != nullptr) {
             const uint4 t = *at;
             const uint32_t w[4] = {t.x, t.y, t.z, t.w};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (F32) v[e] += __uint_as_float(w[e]);
-              else { v[(2 * e) % kPiece] += bf16_lo(w[e]); v[(2 * e + 1) % kPiece] += bf16_hi(w[e]); }
+            for (int i = 0; i < 4; ++i) {
+              if constexpr (F32) e[i] += __uint_as_float(w[i]);
+              else { e[2 * i] += bf16_lo(w[i]); e[2 * i + 1] += bf16_hi(w[i]); }
             }
           }
-          if (F32) *at = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-          else *at = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4 % kPiece], v[5 % kPiece]), pack_bf16x2(v[6 % kPiece], v[7 % kPiece]));
+          if constexpr (F32) *at = make_uint4(__float_as_uint(e[0]), __float_as_uint(e[1]), __float_as_uint(e[2]), __float_as_uint(e[3]));
+          else *at = make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7]));
         }
-        tc::fence_proxy_async_smem();
-        tc::named_bar_sync(1 + group, 128);
-        if (issuer) {
-          if (m0 < p.M && n0 + c * kCols < p.N) tc::tma_store_2d(&map_y, buf, n0 + c * kCols, m0);
-          tc::bulk_commit();
+        if ((h + 1) * 32 % kCols != 0) continue;
+        const int first = n0 + (F32 ? 32 * h : 0);          // column of the 4 KB
+        if (WIDE) {
+          tc::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (in && first < p.N) tc::tma_store_2d(&map_y, turn, first, m0);
+            tc::bulk_commit();
+          }
+        } else {
+          __syncwarp();
+          if (in) {
+#pragma unroll 4
+            for (int row = 0; row < 32; ++row) {
+              char* at = reinterpret_cast<char*>(p.y) + ((int64_t)(m0 + row) * p.ldy + first) * kSize;
+              for (int c = lane; c < kCols; c += 32) {
+                if (m0 + row >= p.M || first + c >= p.N) continue;
+                if (F32) reinterpret_cast<uint32_t*>(at)[c] = *reinterpret_cast<const uint32_t*>(element(row, c));
+                else reinterpret_cast<uint16_t*>(at)[c] = *reinterpret_cast<const uint16_t*>(element(row, c));
+              }
+            }
+          }
         }
       }
     }
-    if (issuer) tc::bulk_wait_all();
+    if (WIDE && lane == 0) tc::bulk_wait_all();
   }
   // neither CTA may leave while its peer can still read its shared memory or arrive on its barriers
   tc::tc_fence_before();
@@ -502,9 +620,8 @@ static grace_status_t launch_act(const CUtensorMap& mx, const CUtensorMap& mw, c
   return GRACE_OK;
 }
 
-template <bool F8, bool F32>
-static grace_status_t launch_act_pair(const CUtensorMap& mx, const CUtensorMap& mw, const CUtensorMap& my, const CUtensorMap& mr,
-                                      const ActParams& p, cudaStream_t s) {
+template <bool F8, bool F32, bool WIDE>
+static grace_status_t launch_act_pair(const CUtensorMap& mx, const CUtensorMap& mw, const CUtensorMap& my, const ActParams& p, cudaStream_t s) {
   static unsigned long long attr_set_devices = 0;
   static int max_clusters_of[kMaxDevices] = {0};
   cudaLaunchConfig_t cfg = {};
@@ -516,11 +633,11 @@ static grace_status_t launch_act_pair(const CUtensorMap& mx, const CUtensorMap& 
   cfg.blockDim = dim3(kAPThreads); cfg.dynamicSmemBytes = kAPSmem; cfg.stream = s; cfg.attrs = attr; cfg.numAttrs = 2;
   DeviceSetup su(&attr_set_devices);
   if (su) {
-    GRACE_CUDA_TRY(cudaFuncSetAttribute(act_pair_kernel<F8, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAPSmem));
+    GRACE_CUDA_TRY(cudaFuncSetAttribute(act_pair_kernel<F8, F32, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAPSmem));
     int n_sm = 0, clusters = 0;
     GRACE_CUDA_TRY(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, su.dev));
     cfg.gridDim = dim3(n_sm & ~1);
-    GRACE_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, act_pair_kernel<F8, F32>, &cfg));
+    GRACE_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, act_pair_kernel<F8, F32, WIDE>, &cfg));
     if (clusters <= 0) return GRACE_CUDA_ERROR;
     max_clusters_of[su.dev] = clusters < n_sm / 2 ? clusters : n_sm / 2;
     su.done();
@@ -528,7 +645,7 @@ static grace_status_t launch_act_pair(const CUtensorMap& mx, const CUtensorMap& 
   const int64_t total = (int64_t)((p.N + 255) / 256) * ((p.M + 255) / 256);
   const int most = max_clusters_of[su.dev];
   cfg.gridDim = dim3(2 * (unsigned)(total < most ? total : most));
-  GRACE_CUDA_TRY(cudaLaunchKernelEx(&cfg, act_pair_kernel<F8, F32>, mx, mw, my, mr, p));
+  GRACE_CUDA_TRY(cudaLaunchKernelEx(&cfg, act_pair_kernel<F8, F32, WIDE>, mx, mw, my, p));
   GRACE_LAUNCH_CHECK();
   return GRACE_OK;
 }
@@ -570,25 +687,21 @@ static grace_status_t linear_act_impl(const void* x, int64_t ldx, const float* x
   p.x_scale = x_scale; p.w_scale = w_scale; p.bias = bias; p.residual = residual; p.y = y;
   p.ldr = ldr; p.ldy = ldy; p.M = M; p.N = N; p.KB = (K + kBK - 1) / kBK; p.act = act;
   cudaStream_t s = (cudaStream_t)stream;
-  // The pair kernel moves y and the residual by TMA: rows that start on 16 bytes.
-  const bool tma_rows = ((reinterpret_cast<uintptr_t>(y) | (uintptr_t)(ldy * size)) & 15) == 0 &&
-                        (residual == nullptr || ((reinterpret_cast<uintptr_t>(residual) | (uintptr_t)(ldr * size)) & 15) == 0);
-  const bool pair_possible = linear_pair_possible(M, N, !tma_rows);
-  if (!pair_possible && (M + kGemmBM - 1) / kGemmBM > 65535) return GRACE_UNSUPPORTED_SHAPE;
-  const LinearForm form = linear_form(M, N, p.KB * kGemmBK, pair_possible, kStatsNone, false);
+  const LinearForm form = linear_form(M, N, p.KB * kGemmBK, linear_pair_possible(M, N, false), kStatsNone, false);
   const CUtensorMapDataType type = F8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   CUtensorMap mx, mw;
   const uint64_t dx[2] = {(uint64_t)K, (uint64_t)M}, sx[1] = {(uint64_t)ldx}, dw[2] = {(uint64_t)K, (uint64_t)N}, sw[1] = {(uint64_t)ldw};
   const uint32_t bx[2] = {(uint32_t)kBK, 128u}, bw[2] = {(uint32_t)kBK, form.bn == 0 ? 128u : (uint32_t)form.bn};
   if (!tc::make_tmap_typed(&mx, x, 2, dx, sx, bx, type, kEsize) || !tc::make_tmap_typed(&mw, w, 2, dw, sw, bw, type, kEsize)) return GRACE_CUDA_ERROR;
   if (form.bn != 0) return f32 ? run_act<F8, true>(form, mx, mw, p, s) : run_act<F8, false>(form, mx, mw, p, s);
-  CUtensorMap my, mr;
-  const uint64_t dy[2] = {(uint64_t)N, (uint64_t)M}, sy[1] = {(uint64_t)ldy}, sr[1] = {(uint64_t)ldr};
-  const uint32_t by[2] = {f32 ? 32u : 64u, 128u};
-  if (!tc::make_tmap(&my, y, 2, dy, sy, by, f32)) return GRACE_CUDA_ERROR;
-  mr = my;
-  if (residual != nullptr && !tc::make_tmap(&mr, residual, 2, dy, sr, by, f32)) return GRACE_CUDA_ERROR;
-  return f32 ? launch_act_pair<F8, true>(mx, mw, my, mr, p, s) : launch_act_pair<F8, false>(mx, mw, my, mr, p, s);
+  const bool wide = ((reinterpret_cast<uintptr_t>(y) | (uintptr_t)(ldy * size)) & 15) == 0 &&
+                    (residual == nullptr || ((reinterpret_cast<uintptr_t>(residual) | (uintptr_t)(ldr * size)) & 15) == 0);
+  CUtensorMap my = mx;                                     // read with `wide` alone
+  const uint64_t dy[2] = {(uint64_t)N, (uint64_t)M}, sy[1] = {(uint64_t)ldy};
+  const uint32_t by[2] = {f32 ? 32u : 64u, 32u};
+  if (wide && !tc::make_tmap(&my, y, 2, dy, sy, by, f32)) return GRACE_CUDA_ERROR;
+  if (f32) return wide ? launch_act_pair<F8, true, true>(mx, mw, my, p, s) : launch_act_pair<F8, true, false>(mx, mw, my, p, s);
+  return wide ? launch_act_pair<F8, false, true>(mx, mw, my, p, s) : launch_act_pair<F8, false, false>(mx, mw, my, p, s);
 }
 int linear_act_tc_timeouts() { return tc::tc_timeouts_read_and_clear(); }
 

@@ -165,14 +165,6 @@ __device__ __forceinline__ void named_bar_sync(int id, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
 }
 
-// The same barrier; true if `ok` is true in all of its threads.
-__device__ __forceinline__ bool named_bar_and(int id, int threads, bool ok) {
-  uint32_t all;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbar.red.and.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(all) : "r"(id), "r"(threads), "r"((uint32_t)ok) : "memory");
-  return all != 0;
-}
-
 __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap* map) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
 }
