@@ -82,26 +82,6 @@ __device__ __forceinline__ void act_all(float (&v)[N], int act) {
   }
 }
 
-// v = acc * xs * scale + bias of 32 columns, whose scales and biases (64 floats behind the scales) lie in shared memory.
-template <bool F8>
-__device__ __forceinline__ void act_affine(float (&v)[32], const uint32_t (&acc)[32], float xs, const float* scale) {
-  const f32x2_t x2 = f2_pack(xs, xs);
-#pragma unroll
-  for (int i = 0; i < 32; i += 4) {
-    const float4 b4 = *reinterpret_cast<const float4*>(scale + 64 + i);
-    f32x2_t lo = f2_pack(__uint_as_float(acc[i]), __uint_as_float(acc[i + 1])), hi = f2_pack(__uint_as_float(acc[i + 2]), __uint_as_float(acc[i + 3]));
-    if (F8) {
-      const float4 s4 = *reinterpret_cast<const float4*>(scale + i);
-      lo = f2_fma(f2_mul(lo, x2), f2_pack(s4.x, s4.y), f2_pack(b4.x, b4.y));
-      hi = f2_fma(f2_mul(hi, x2), f2_pack(s4.z, s4.w), f2_pack(b4.z, b4.w));
-    } else {
-      lo = f2_add(lo, f2_pack(b4.x, b4.y));
-      hi = f2_add(hi, f2_pack(b4.z, b4.w));
-    }
-    f2_unpack(lo, v[i], v[i + 1]);
-    f2_unpack(hi, v[i + 2], v[i + 3]);
-  }
-}
 template <bool F8, bool PAIR>
 __device__ __forceinline__ void act_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   if (PAIR) {
@@ -342,22 +322,44 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 // ---------------------------------------------------------------------------------------------
 // Persistent CTA pairs: 256 x 256 tiles (n fastest), each CTA with 128 rows of x and 128 of the tile's rows of w in a ring of
 // five stages, one tcgen05.mma stream per pair into one of two accumulators (all of TMEM).
-// Epilogue: sixteen warps per CTA, each with 32 rows x 64 columns of its own.  A thread has a row: it takes 32 columns at a
-// time out of the accumulator, finishes them and leaves them in the warp's 4 KB of shared memory (128 bytes a row, swizzled),
-// from where a TMA store takes them.  The residual comes the same way: whole row segments into registers while the warp waits
-// for the accumulator, from there into the 4 KB, and a thread adds its row's where the results will lie.  No warp waits for
-// another.  WIDE: rows of y and of the residual start on 16 bytes; otherwise
-// the warp moves single elements between the 4 KB and memory.
+// Epilogue: sixteen warps per CTA, each with 32 rows x 64 columns of its own.  A thread has a row: it takes a step's columns
+// (32 of a bf16 result, 16 of an fp32 one) out of the accumulator, finishes them and leaves them in the warp's 2 KB of shared
+// memory (64 bytes a row, swizzled), from where a TMA store takes them.  The residual comes the same way: row segments into
+// registers one step ahead, from there into the 2 KB, and a thread adds its row's where the results will lie.  No warp waits
+// for another.  WIDE: rows of y and of the residual start on 16 bytes; otherwise the warp moves single elements between the
+// 2 KB and memory.
 // (Eight warps in two groups that share a buffer and its barriers: 84 us for 65536 x 2048 x 512 in e4m3, without activation.)
 // ---------------------------------------------------------------------------------------------
-constexpr int kAPStages = 4;
+constexpr int kAPStages = 5;
 constexpr int kAPStageBytes = 2 * 128 * 128;
-constexpr int kAPWarps = 16;
-constexpr int kAPTurn = 32 * 128;                          // 32 rows of 64 bf16 or 32 fp32
-constexpr int kAPCols = 2 * 64 * 4;                         // scales and biases of the warp's 64 columns
+constexpr int kAPWarps = 16, kAPWarpCols = 64;             // columns of a tile that a warp finishes
+constexpr int kAPRow = 64;                                 // bytes of a row in a warp's shared memory
+constexpr int kAPTurn = 32 * kAPRow;
+constexpr int kAPCols = 2 * kAPWarpCols * 4;               // scales and biases of the warp's columns
 constexpr int kAPSmem = kAPStages * kAPStageBytes + kAPWarps * (kAPTurn + kAPCols) + 256;
 constexpr int kAPThreads = 64 + 32 * kAPWarps;
 static_assert(kAPSmem >= tc::kTmemAllSmem && kAPSmem <= 227 * 1024, "");
+
+// v = acc * xs * scale + bias of N columns, whose scales and biases (kAPWarpCols behind the scales) lie in shared memory.
+template <bool F8, int N>
+__device__ __forceinline__ void act_affine(float (&v)[N], const uint32_t (&acc)[N], float xs, const float* scale) {
+  const f32x2_t x2 = f2_pack(xs, xs);
+#pragma unroll
+  for (int i = 0; i < N; i += 4) {
+    const float4 b4 = *reinterpret_cast<const float4*>(scale + kAPWarpCols + i);
+    f32x2_t lo = f2_pack(__uint_as_float(acc[i]), __uint_as_float(acc[i + 1])), hi = f2_pack(__uint_as_float(acc[i + 2]), __uint_as_float(acc[i + 3]));
+    if (F8) {
+      const float4 s4 = *reinterpret_cast<const float4*>(scale + i);
+      lo = f2_fma(f2_mul(lo, x2), f2_pack(s4.x, s4.y), f2_pack(b4.x, b4.y));
+      hi = f2_fma(f2_mul(hi, x2), f2_pack(s4.z, s4.w), f2_pack(b4.z, b4.w));
+    } else {
+      lo = f2_add(lo, f2_pack(b4.x, b4.y));
+      hi = f2_add(hi, f2_pack(b4.z, b4.w));
+    }
+    f2_unpack(lo, v[i], v[i + 1]);
+    f2_unpack(hi, v[i + 2], v[i + 3]);
+  }
+}
 
 template <bool F8, bool F32, bool WIDE>
 __global__ void __launch_bounds__(kAPThreads, 1)
@@ -444,19 +446,20 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     }
   } else {
     // ---- epilogue warps 2..17: rows q*32 .. of this CTA's 128 (q: the warp's TMEM lane quarter), 64 columns ----
-    const int q = warp & 3, col = ((warp - 2) >> 2) * 64;
-    uint8_t* const turn = turns + (warp - 2) * kAPTurn;     // [32 rows][8 pieces of 16 bytes], swizzled by the row
-    uint4* const my_row = reinterpret_cast<uint4*>(turn + lane * 128);
-    constexpr int kSize = F32 ? 4 : 2, kPer = 16 / kSize, kCols = 128 / kSize;  // columns of a piece, of the 4 KB
-    auto element = [&](int row, int c) { return turn + row * 128 + (((c / kPer) ^ (row & 7)) << 4) + (c % kPer) * kSize; };
-    uint4 held[8];                                          // the residual of the next kCols columns
+    const int q = warp & 3, col = ((warp - 2) >> 2) * kAPWarpCols;
+    constexpr int kSize = F32 ? 4 : 2, kPer = 16 / kSize, kCols = kAPRow / kSize;   // columns of a piece, of a step
+    constexpr int kPieces = kAPRow / 16, kRows = 32 / kPieces;  // of a row; rows of 32 pieces
+    uint8_t* const turn = turns + (warp - 2) * kAPTurn;     // [32 rows][kPieces], swizzled by the row
+    auto piece = [&](int row, int j) { return reinterpret_cast<uint4*>(turn + row * kAPRow + ((j ^ ((row >> 1) & 3)) << 4)); };
+    auto element = [&](int row, int c) { return reinterpret_cast<uint8_t*>(piece(row, c / kPer)) + (c % kPer) * kSize; };
+    uint4 held[kPieces];                                    // the residual of the next step's columns
     auto hold = [&](int m0, int n0) {
+      const int m = m0 + lane / kPieces, n = n0 + lane % kPieces * kPer;
+      const char* at = reinterpret_cast<const char*>(p.residual) + ((int64_t)m * p.ldr + n) * kSize;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int m = m0 + 4 * i + (lane >> 3), n = n0 + (lane & 7) * kPer;
+      for (int i = 0; i < kPieces; ++i, at += kRows * p.ldr * kSize) {
         held[i] = make_uint4(0, 0, 0, 0);
-        if (WIDE && m < p.M && n < p.N) {                   // (not .nc: the residual may be y itself)
-          const char* at = reinterpret_cast<const char*>(p.residual) + ((int64_t)m * p.ldr + n) * kSize;
+        if (m + kRows * i < p.M && n < p.N) {                   // (not .nc: the residual may be y itself)
           if (n + kPer <= p.N) {
             held[i] = *reinterpret_cast<const uint4*>(at);
           } else {
@@ -474,69 +477,52 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     };
     // the row's scale and the columns' vectors, one tile ahead; the latter in a copy of the warp's own
     float* const scale = reinterpret_cast<float*>(turns + kAPWarps * kAPTurn + (warp - 2) * kAPCols);
-    float xs_next = 1.f, col_next[4] = {1.f, 1.f, 0.f, 0.f};
-    auto fetch = [&](int tile) {
-      tile = min(tile, total - 1);
-      const int m = min((tile / n_tiles) * 256 + (int)rank * 128 + q * 32 + lane, p.M - 1), n = (tile % n_tiles) * 256 + col + lane;
-      if (F8 && p.x_scale != nullptr) xs_next = __ldg(p.x_scale + m);
+    constexpr int kVec = kAPWarpCols / 32;
+    float xs_next = 1.f, ws_next[kVec], bias_next[kVec];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (F8 && p.w_scale != nullptr) col_next[i] = __ldg(p.w_scale + min(n + 32 * i, p.N - 1));
-        if (p.bias != nullptr) col_next[2 + i] = __ldg(p.bias + min(n + 32 * i, p.N - 1));
+    for (int i = 0; i < kVec; ++i) { ws_next[i] = 1.f; bias_next[i] = 0.f; }
+    auto fetch = [&](int m0, int n0) {
+      if (F8 && p.x_scale != nullptr) xs_next = __ldg(p.x_scale + min(m0 + lane, p.M - 1));
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        const int n = min(n0 + 32 * i + lane, p.N - 1);
+        if (F8 && p.w_scale != nullptr) ws_next[i] = __ldg(p.w_scale + n);
+        if (p.bias != nullptr) bias_next[i] = __ldg(p.bias + n);
       }
     };
-    fetch(pair);
+    // the next tile's coordinates without a division
+    const int step_m = n_pairs / n_tiles, step_n = n_pairs % n_tiles;
+    int tile_m = pair / n_tiles, tile_n = pair % n_tiles;
+    int m0 = tile_m * 256 + (int)rank * 128 + q * 32, n0 = tile_n * 256 + col;
+    fetch(m0, n0);
     int local = 0;
     for (int tile = pair; tile < total; tile += n_pairs, ++local) {
-      const int m0 = (tile / n_tiles) * 256 + (int)rank * 128 + q * 32, n0 = (tile % n_tiles) * 256 + col;
+      m0 = tile_m * 256 + (int)rank * 128 + q * 32;
+      n0 = tile_n * 256 + col;
+      tile_m += step_m;
+      tile_n += step_n;
+      if (tile_n >= n_tiles) { tile_n -= n_tiles; ++tile_m; }
       const int ab = local & 1;
       if (WIDE && p.residual != nullptr) hold(m0, n0);
       const float xs = xs_next;
       __syncwarp();                                         // the tile in front has been finished with them
 #pragma unroll
-      for (int i = 0; i < 4; ++i) scale[32 * i + lane] = col_next[i];
-      fetch(tile + n_pairs);
+      for (int i = 0; i < kVec; ++i) {
+        if (F8) scale[32 * i + lane] = ws_next[i];
+        scale[kAPWarpCols + 32 * i + lane] = bias_next[i];
+      }
+      fetch(tile_m * 256 + (int)rank * 128 + q * 32, tile_n * 256 + col);
       bool ok = tc::mbar_wait_cluster(acc_full + ab, (local >> 1) & 1, abort_flag);
       ok = __all_sync(kFullMask, ok);
       if (!ok) break;
       tc::tc_fence_after();
       const uint32_t t_acc = tmem_base + (uint32_t)(ab * 256 + col) + ((uint32_t)(q * 32) << 16);
-      const bool in = m0 < p.M;
 #pragma unroll 1
-      for (int h = 0; h < 2; ++h) {
-        if (h * 32 % kCols == 0) {                          // a new filling of the 4 KB
-          if (WIDE) {
-            if (lane == 0) tc::bulk_wait_read<0>();
-            __syncwarp();
-            if (p.residual != nullptr) {
-#pragma unroll
-              for (int i = 0; i < 8; ++i) {
-                const int row = 4 * i + (lane >> 3);
-                *reinterpret_cast<uint4*>(turn + row * 128 + (((lane & 7) ^ (row & 7)) << 4)) = held[i];
-              }
-              if (kCols == 32 && h == 0) hold(m0, n0 + 32);
-              __syncwarp();
-            }
-          } else {
-            __syncwarp();
-            if (p.residual != nullptr && in) {
-#pragma unroll 4
-              for (int row = 0; row < 32; ++row) {
-                const char* at = reinterpret_cast<const char*>(p.residual) + ((int64_t)(m0 + row) * p.ldr + n0 + 32 * h) * kSize;
-                for (int c = lane; c < kCols; c += 32) {
-                  if (m0 + row >= p.M || n0 + 32 * h + c >= p.N) continue;
-                  if (F32) *reinterpret_cast<uint32_t*>(element(row, c)) = reinterpret_cast<const uint32_t*>(at)[c];
-                  else *reinterpret_cast<uint16_t*>(element(row, c)) = reinterpret_cast<const uint16_t*>(at)[c];
-                }
-              }
-              __syncwarp();
-            }
-          }
-        }
-        uint32_t r[32];
-        tc::tmem_ld32(t_acc + 32 * h, r);
+      for (int c0 = 0; c0 < kAPWarpCols; c0 += kCols) {
+        uint32_t r[kCols];
+        if constexpr (F32) tc::tmem_ld16(t_acc + c0, r); else tc::tmem_ld32(t_acc + c0, r);
         tc::tmem_ld_wait();
-        if (h == 1) {                                       // this part of the accumulator has been read
+        if (c0 + kCols == kAPWarpCols) {                             // this part of the accumulator has been read
           tc::tc_fence_before();
           __syncwarp();
           if (lane == 0) {
@@ -544,12 +530,35 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             else tc::mbar_arrive_remote(acc_empty + ab, 0);
           }
         }
-        float v[32];
-        act_affine<F8>(v, r, xs, scale + 32 * h);
+        if (m0 >= p.M || n0 + c0 >= p.N) continue;          // the same for the whole warp
+        float v[kCols];
+        act_affine<F8>(v, r, xs, scale + c0);
         act_all<F32>(v, p.act);
+        if (WIDE) {
+          if (lane == 0) tc::bulk_wait_read<0>();           // the step in front has left the 2 KB
+        }
+        __syncwarp();
+        if (p.residual != nullptr) {
+          if (WIDE) {
 #pragma unroll
-        for (int j = 0; j < 32 / kPer; ++j) {
-          uint4* at = my_row + (((h * 32 % kCols) / kPer + j) ^ (lane & 7));
+            for (int i = 0; i < kPieces; ++i) *piece(kRows * i + lane / kPieces, lane % kPieces) = held[i];
+            if (c0 + kCols < kAPWarpCols) hold(m0, n0 + c0 + kCols);
+          } else {
+            const int c = lane % kCols, rows = min(32, p.M - m0);
+            if (n0 + c0 + c < p.N) {
+              const char* at = reinterpret_cast<const char*>(p.residual) + ((int64_t)(m0 + lane / kCols) * p.ldr + n0 + c0 + c) * kSize;
+#pragma unroll 8
+              for (int row = lane / kCols; row < rows; row += 32 / kCols, at += (32 / kCols) * p.ldr * kSize) {
+                if (F32) *reinterpret_cast<uint32_t*>(element(row, c)) = *reinterpret_cast<const uint32_t*>(at);
+                else *reinterpret_cast<uint16_t*>(element(row, c)) = *reinterpret_cast<const uint16_t*>(at);
+              }
+            }
+          }
+          __syncwarp();
+        }
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+          uint4* at = piece(lane, j);
           float* e = v + kPer * j;
           if (p.residual != nullptr) {
             const uint4 t = *at;
@@ -563,26 +572,22 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           if constexpr (F32) *at = make_uint4(__float_as_uint(e[0]), __float_as_uint(e[1]), __float_as_uint(e[2]), __float_as_uint(e[3]));
           else *at = make_uint4(pack_bf16x2(e[0], e[1]), pack_bf16x2(e[2], e[3]), pack_bf16x2(e[4], e[5]), pack_bf16x2(e[6], e[7]));
         }
-        if ((h + 1) * 32 % kCols != 0) continue;
-        const int first = n0 + (F32 ? 32 * h : 0);          // column of the 4 KB
         if (WIDE) {
           tc::fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            if (in && first < p.N) tc::tma_store_2d(&map_y, turn, first, m0);
+            tc::tma_store_2d(&map_y, turn, n0 + c0, m0);
             tc::bulk_commit();
           }
         } else {
           __syncwarp();
-          if (in) {
-#pragma unroll 4
-            for (int row = 0; row < 32; ++row) {
-              char* at = reinterpret_cast<char*>(p.y) + ((int64_t)(m0 + row) * p.ldy + first) * kSize;
-              for (int c = lane; c < kCols; c += 32) {
-                if (m0 + row >= p.M || first + c >= p.N) continue;
-                if (F32) reinterpret_cast<uint32_t*>(at)[c] = *reinterpret_cast<const uint32_t*>(element(row, c));
-                else reinterpret_cast<uint16_t*>(at)[c] = *reinterpret_cast<const uint16_t*>(element(row, c));
-              }
+          const int c = lane % kCols, rows = min(32, p.M - m0);
+          if (n0 + c0 + c < p.N) {
+            char* at = reinterpret_cast<char*>(p.y) + ((int64_t)(m0 + lane / kCols) * p.ldy + n0 + c0 + c) * kSize;
+#pragma unroll 8
+            for (int row = lane / kCols; row < rows; row += 32 / kCols, at += (32 / kCols) * p.ldy * kSize) {
+              if (F32) *reinterpret_cast<uint32_t*>(at) = *reinterpret_cast<const uint32_t*>(element(row, c));
+              else *reinterpret_cast<uint16_t*>(at) = *reinterpret_cast<const uint16_t*>(element(row, c));
             }
           }
         }
@@ -698,8 +703,10 @@ static grace_status_t linear_act_impl(const void* x, int64_t ldx, const float* x
                     (residual == nullptr || ((reinterpret_cast<uintptr_t>(residual) | (uintptr_t)(ldr * size)) & 15) == 0);
   CUtensorMap my = mx;                                     // read with `wide` alone
   const uint64_t dy[2] = {(uint64_t)N, (uint64_t)M}, sy[1] = {(uint64_t)ldy};
-  const uint32_t by[2] = {f32 ? 32u : 64u, 32u};
-  if (wide && !tc::make_tmap(&my, y, 2, dy, sy, by, f32)) return GRACE_CUDA_ERROR;
+  const uint32_t by[2] = {(uint32_t)(kAPRow / size), 32u};
+  if (wide && !tc::make_tmap_typed(&my, y, 2, dy, sy, by, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, size,
+                                   CU_TENSOR_MAP_SWIZZLE_64B))
+    return GRACE_CUDA_ERROR;
   if (f32) return wide ? launch_act_pair<F8, true, true>(mx, mw, my, p, s) : launch_act_pair<F8, true, false>(mx, mw, my, p, s);
   return wide ? launch_act_pair<F8, false, true>(mx, mw, my, p, s) : launch_act_pair<F8, false, false>(mx, mw, my, p, s);
 }

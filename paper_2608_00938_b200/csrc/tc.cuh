@@ -31,9 +31,10 @@ inline EncodeTiledFn encode_tiled_fn() {
 }
 
 // Tensor of `rank` dims (dims[0] innermost, contiguous) of elements of `esize` bytes, strides in elements for dims 1..,
-// box in elements.  128-byte swizzle: box[0] must be 128 bytes.  Out-of-range reads give 0.
+// box in elements.  A swizzle of n bytes: box[0] must be n bytes.  Out-of-range reads give 0.
 inline bool make_tmap_typed(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides_elems,
-                            const uint32_t* box, CUtensorMapDataType type, uint64_t esize, bool swizzle128 = true) {
+                            const uint32_t* box, CUtensorMapDataType type, uint64_t esize,
+                            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   EncodeTiledFn fn = encode_tiled_fn();
   if (fn == nullptr) return false;
   cuuint64_t gdim[5], gstr[4];
@@ -41,15 +42,15 @@ inline bool make_tmap_typed(CUtensorMap* map, const void* base, int rank, const 
   for (int i = 0; i < rank; ++i) { gdim[i] = dims[i]; gbox[i] = box[i]; estr[i] = 1; }
   for (int i = 0; i + 1 < rank; ++i) gstr[i] = strides_elems[i] * esize;
   CUresult r = fn(map, type, (cuuint32_t)rank,
-                  const_cast<void*>(base), gdim, gstr, gbox, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                  const_cast<void*>(base), gdim, gstr, gbox, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   return r == CUDA_SUCCESS;
 }
 inline bool make_tmap(CUtensorMap* map, const void* base, int rank, const uint64_t* dims,
                       const uint64_t* strides_elems, const uint32_t* box, bool is_f32, bool swizzle128 = true) {
   return make_tmap_typed(map, base, rank, dims, strides_elems, box,
-                         is_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, is_f32 ? 4 : 2, swizzle128);
+                         is_f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, is_f32 ? 4 : 2,
+                         swizzle128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 inline bool make_tmap_bf16(CUtensorMap* map, const void* base, int rank, const uint64_t* dims,
                            const uint64_t* strides_elems, const uint32_t* box, bool swizzle128 = true) {
