@@ -1,0 +1,968 @@
+// Tokens drawn from a row's (allowed) logits: temperature, top-k, top-p, min-p, one uniform number per draw.
+//
+//   w_v = e^((x_v - max) / T) over the allowed tokens, in the order (x descending, token ascending).  Every limit leaves a
+//   prefix of that order, so what is kept is a cut (t, i): tokens with x > t, and of those with x = t the ones up to token i.
+//   A draw takes the first kept token, in ascending order, at which the running sum of kept weights exceeds u times the whole.
+//
+// A warp has a row of up to 2048 tokens, a CTA a longer one (or one of few).  A pass or two over the row leave a list of the
+// elements that can be kept: those of at least min-p's bound, of the histogram steps down to the one that holds the top_k-th, or
+// heavy enough for top-p (a set whose weights are all at most (1 - p) S / n weighs at most (1 - p) S, so nothing of it is
+// needed to reach p S).  With a constraint the list is the allowed tokens.  Everything else happens on the list, in shared
+// memory.  The loops are rolled: unrolled over a row in registers, the same steps waited for instructions six cycles of
+// fourteen.
+// No sort: the cut is found through a histogram of 256 equal steps of (max - x) / T, in counts (top-k) or in fixed-point
+// weights (top-p), whose one step that holds the cut is then resolved value by value.
+// The answer is that of the definition in 64 bits, at the cost of 32: weights and sums are fp32, every comparison of a sum with
+// a border has a margin above the sums' worst error, and a row for which one falls inside the margin is done again with
+// e^ and sums in fp64.
+#pragma once
+
+#include "common.cuh"
+
+namespace grace {
+
+struct SampleParams {
+  const void* logits;            // fp32 or bf16 [R][ld]
+  const uint64_t* allow;         // [R][words] or NULL
+  const float *row_score, *row_lse;                        // [R] or NULL
+  const float* temperature;      // [B] or NULL, as the next three
+  const int32_t* top_k;
+  const float *top_p, *min_p;
+  const float* u;                // [R][draws]
+  float *out_score, *out_logq;   // [R][draws]
+  int32_t *out_parent, *out_token;
+  int32_t* d_status;
+  int64_t ld, R;
+  int M, V, draws, vec;          // vec: quads of a row lie on their own size
+  int cap;                       // elements that a row's list takes, a multiple of 16
+  int team_bytes;                // shared memory of a team
+};
+
+constexpr int kSampleBuckets = 256;
+// Steps of the histogram: 256 over 22 powers of two of weight; the last one holds all that is lighter.
+constexpr float kSampleSteps = 256.f / 22.f;
+constexpr int kSampleMostV = 65536;
+
+__device__ __forceinline__ float sample_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// The larger of two values, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// The threads that share a row: a warp, or a CTA.
+template <int NW>
+struct Team {
+  static constexpr int NT = NW * 32;
+  int tid;
+  double* red;                                             // [NW] shared, NW > 1
+  __device__ __forceinline__ void sync() const {
+    if (NW == 1) __syncwarp(); else __syncthreads();
+  }
+  template <class T, class Op>
+  __device__ __forceinline__ T reduce(T v, Op op) const {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(kFullMask, v, o));
+    if (NW > 1) {
+      T* r = reinterpret_cast<T*>(red);
+      __syncthreads();
+      if ((tid & 31) == 0) r[tid >> 5] = v;
+      __syncthreads();
+      v = r[(tid & 31) & (NW - 1)];
+#pragma unroll
+      for (int o = NW / 2; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(kFullMask, v, o));
+    }
+    return v;
+  }
+  template <class T> __device__ __forceinline__ T sum(T v) const { return reduce(v, [](T a, T b) { return a + b; }); }
+  __device__ __forceinline__ int sum(int v) const {
+    if (NW == 1) return __reduce_add_sync(kFullMask, v);
+    return reduce(v, [](int a, int b) { return a + b; });
+  }
+  // inclusive prefix sum over the threads
+  template <class T>
+  __device__ __forceinline__ T scan(T v) const {
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const T t = __shfl_up_sync(kFullMask, v, o);
+      if ((tid & 31) >= o) v += t;
+    }
+    if (NW > 1) {
+      T* r = reinterpret_cast<T*>(red);
+      __syncthreads();
+      if ((tid & 31) == 31) r[tid >> 5] = v;
+      __syncthreads();
+      T before = T(0);
+      for (int w = 0; w < (tid >> 5); ++w) before += r[w];
+      v += before;
+    }
+    return v;
+  }
+};
+
+template <bool BF16>
+__device__ __forceinline__ float logit_at(const char* row, int token) {
+  return BF16 ? __uint_as_float((uint32_t)__ldg(reinterpret_cast<const uint16_t*>(row) + token) << 16) : __ldg(reinterpret_cast<const float*>(row) + token);
+}
+
+// A row's elements in the order of their tokens: in shared memory (`tokens` NULL: element i is token i), ...
+struct RowShared {
+  const float* vals;
+  const uint16_t* tokens;
+  int n;
+  __device__ __forceinline__ float at(int i) const { return vals[i]; }
+  __device__ __forceinline__ int token(int i) const { return tokens != nullptr ? tokens[i] : i; }
+};
+// ... or where they are, read again by every pass (out of L2): a row of which more stays than a list takes.
+template <bool BF16>
+struct RowGlobal {
+  const char* row;
+  const uint64_t* allow;
+  int n, vec;
+  bool inf;                      // the row's largest is +inf: these weigh 1, all others nothing
+  __device__ __forceinline__ float shown(float x) const { return inf ? (x == INFINITY ? 0.f : -INFINITY) : x; }
+  __device__ __forceinline__ float at(int i) const {
+    if (allow != nullptr && !((__ldg(allow + (i >> 6)) >> (i & 63)) & 1ull)) return -INFINITY;
+    return shown(logit_at<BF16>(row, i));
+  }
+  __device__ __forceinline__ int token(int i) const { return i; }
+  // elements 4q ..: -inf where they are not allowed or beyond the row
+  __device__ __forceinline__ float4 quad(int q) const {
+    const int i = q << 2;
+    if (allow == nullptr && vec && i + 4 <= n && !inf) return whole_quad(q);
+    uint32_t bits = allow != nullptr ? (uint32_t)(__ldg(allow + (i >> 6)) >> (i & 63)) & 15u : 15u;
+    if (i + 4 > n) bits &= (1u << (n - i)) - 1u;
+    float4 t = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    if (bits == 0u) return t;
+    if (vec && i + 4 <= n) {
+      t = whole_quad(q);
+    } else {
+      if (bits & 1u) t.x = logit_at<BF16>(row, i);
+      if (bits & 2u) t.y = logit_at<BF16>(row, i + 1);
+      if (bits & 4u) t.z = logit_at<BF16>(row, i + 2);
+      if (bits & 8u) t.w = logit_at<BF16>(row, i + 3);
+    }
+    t.x = (bits & 1u) ? shown(t.x) : -INFINITY;
+    t.y = (bits & 2u) ? shown(t.y) : -INFINITY;
+    t.z = (bits & 4u) ? shown(t.z) : -INFINITY;
+    t.w = (bits & 8u) ? shown(t.w) : -INFINITY;
+    return t;
+  }
+  __device__ __forceinline__ float4 whole_quad(int q) const {
+    if (!BF16) return __ldg(reinterpret_cast<const float4*>(row) + q);
+    const uint2 w = __ldg(reinterpret_cast<const uint2*>(row) + q);
+    return make_float4(bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y));
+  }
+};
+// The elements of a row that its list leaves out, those below `bound`: their weight in 64 bits.
+template <bool BF16>
+struct LeftOut {
+  RowGlobal<BF16> row;
+  float bound;
+  template <int NW>
+  __device__ __noinline__ double weight64(const Team<NW>& tm, float m, double inv_t) const {
+    double t = 0.;
+    for (int i = tm.tid; i < row.n; i += NW * 32) {
+      const float x = row.at(i);
+      if (x > -INFINITY && x < bound) t += exp(((double)x - (double)m) * inv_t);
+    }
+    return tm.sum(t);
+  }
+};
+
+struct Cut {
+  float t;                       // x > t, or x = t and place <= last
+  int last;
+  __device__ __forceinline__ bool keeps(float x, int place) const { return x > t || (x == t && place <= last); }
+};
+
+// A team's shared memory, in front of its list (vals [cap], tokens [cap]).
+template <int NW>
+struct SampleShared {
+  static constexpr int kList = NW == 1 ? 64 : 256;         // values of a histogram step that are resolved one by one
+  double table[NW * 128];                                  // sums of weights over groups of elements, four groups a thread
+  double prefix[NW * 32];
+  double red[NW < 2 ? 2 : NW];
+  uint32_t hist[kSampleBuckets];
+  float list[kList];
+  int n_list, bucket, found, found_r;
+  float found_t;
+  uint32_t above;
+  int found_all, place;
+};
+
+// First step at which the histogram's running sum reaches `target` (sh.bucket) and the sum in front of it (sh.above);
+// -1 if none does.
+template <int NW>
+__device__ __forceinline__ void find_bucket(const Team<NW>& tm, SampleShared<NW>& sh, uint32_t target) {
+  if (tm.tid < 32) {
+    const int lane = tm.tid;
+    const uint4 lo = reinterpret_cast<const uint4*>(sh.hist)[2 * lane], hi = reinterpret_cast<const uint4*>(sh.hist)[2 * lane + 1];
+    const uint32_t h[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    const uint32_t s = ((h[0] + h[1]) + (h[2] + h[3])) + ((h[4] + h[5]) + (h[6] + h[7]));
+    uint32_t incl = s;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t t = __shfl_up_sync(kFullMask, incl, o);
+      if (lane >= o) incl += t;
+    }
+    const uint32_t reached = __ballot_sync(kFullMask, incl >= target);
+    if (reached == 0u) {
+      if (lane == 0) sh.bucket = -1;
+    } else if (lane == __ffs(reached) - 1) {
+      uint32_t run = incl - s, front = run;
+      int at = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        run += h[j];
+        if (run < target) { at = j + 1; front = run; }
+      }
+      sh.bucket = 8 * lane + at;
+      sh.above = front;
+    }
+  }
+  tm.sync();
+}
+template <int NW>
+__device__ __forceinline__ void clear_hist(const Team<NW>& tm, SampleShared<NW>& sh) {
+  for (int i = tm.tid; i < kSampleBuckets / 4; i += NW * 32) reinterpret_cast<uint4*>(sh.hist)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
+// The exact work on a row (a list, as a rule).
+template <int NW, class Row, class Rest>
+struct Sampler {
+  const Row& row;
+  const Team<NW>& tm;
+  SampleShared<NW>& sh;
+  float m;                       // largest value
+  float c;                       // log2(e) / T
+  double inv_t;                  // 1 / T
+  float margin;                  // of sums, relative to the whole
+  int group;                     // elements of a table entry
+  // top-p counts elements that the list leaves out: their weight with the list's (0: the row is all there is), and where they are
+  float whole_row;
+  const Rest& rest;
+  static constexpr int NT = NW * 32;
+
+  __device__ __forceinline__ float weight(float x) const { return sample_ex2((x - m) * c); }
+  __device__ __forceinline__ double weight64(float x) const { return exp(((double)x - (double)m) * inv_t); }
+  __device__ __forceinline__ int bucket_of(float x) const { return min(kSampleBuckets - 1, (int)((m - x) * c * kSampleSteps)); }
+  template <class F>
+  __device__ __forceinline__ void for_each(F f) const {
+    for (int i = tm.tid; i < row.n; i += NT) f(row.at(i), i);
+  }
+  __device__ __forceinline__ void note(float t, int r, int same) const {
+    sh.found_t = t; sh.found_r = r; sh.found_all = r == same; sh.found = 1;
+  }
+
+  // Narrows `cut` to its first k elements (MASS false), or to the fewest whose weights reach p of the sum of its weights.
+  template <bool MASS>
+  __device__ __noinline__ Cut narrow(const Cut cut, const int k, const float p) const {
+    // fixed point: the sum of any row below 2^32
+    const float scale = MASS ? exp2f(31.f - ceilf(log2f((float)row.n))) : 1.f;
+    auto share = [&](float x) { return MASS ? __float2uint_rn(weight(x) * scale) : 1u; };
+    tm.sync();
+    clear_hist(tm, sh);
+    if (tm.tid == 0) { sh.n_list = 0; sh.found = 0; }
+    tm.sync();
+    for_each([&](float x, int place) {
+      if (cut.keeps(x, place)) atomicAdd(&sh.hist[bucket_of(x)], share(x));
+    });
+    tm.sync();
+    auto mass_goal = [&](float want) {                     // within what the histogram holds
+      uint32_t all = 0;
+      for (int i = tm.tid; i < kSampleBuckets; i += NT) all += sh.hist[i];
+      all = tm.reduce(all, [](uint32_t a, uint32_t b) { return a + b; });
+      if (want < 0.f) want = (float)all * p;
+      return min(max(1u, (uint32_t)fminf(want, 4294967040.f)), max(1u, all));
+    };
+    find_bucket(tm, sh, MASS ? mass_goal(whole_row > 0.f ? whole_row * scale * p : -1.f) : (uint32_t)k);
+    if (sh.bucket < 0) return cut;                         // no more than k elements
+    const int b = sh.bucket;
+    float whole = 0.f, above = 0.f;
+    int n_above = (int)sh.above;
+    for_each([&](float x, int place) {
+      if (!cut.keeps(x, place)) return;
+      const int at = bucket_of(x);
+      if (MASS) {
+        const float w = weight(x);
+        whole += w;
+        above += at < b ? w : 0.f;
+      }
+      if (at == b) {
+        const int i = atomicAdd(&sh.n_list, 1);
+        if (i < sh.kList) sh.list[i] = x;
+      }
+    });
+    if (MASS) {
+      whole = whole_row > 0.f ? whole_row : tm.sum(whole);
+      above = tm.sum(above);
+    }
+    tm.sync();
+    const int n = sh.n_list;
+    int len = n, copies = 1;
+    if (n > sh.kList) narrow_keys<MASS>(cut, k, p, b, scale, whole, above, n_above, len, copies);
+    // The list resolved: the value at which the count or the sum of weights in front passes the goal.
+    for (int i = tm.tid; i < len; i += NT) {
+      const float x = sh.list[i];
+      int same = 0;
+      if (MASS) {
+        float front = above;
+        for (int j = 0; j < len; ++j) {
+          const float y = sh.list[j];
+          if (y > x) front += weight(y);
+          same += y == x;
+        }
+        same *= copies;
+        const float w = weight(x), gap = p * whole - front, slack = margin * whole;
+        if (gap > slack && gap + slack < w * (float)same) {
+          const float q = gap / w, r = ceilf(q);
+          if (same == 1 || ((r - q) * w > slack && (q - (r - 1.f)) * w > slack)) note(x, min(same, max(1, (int)r)), same);
+        }
+      } else {
+        int front = n_above;
+        for (int j = 0; j < len; ++j) { const float y = sh.list[j]; front += y > x; same += y == x; }
+        same *= copies;
+        if (front < k && k <= front + same) note(x, k - front, same);
+      }
+    }
+    tm.sync();
+    if (MASS && sh.found == 0) narrow64(cut, p, len, copies);
+    Cut out = {sh.found_t, 0x7fffffff};
+    if (sh.found_all != 0) {
+      if (out.t == cut.t) out.last = cut.last;
+      return out;
+    }
+    out.last = nth_tie(cut, out.t, sh.found_r);
+    return out;
+  }
+
+  // Place of the r-th of the elements with value t that `cut` keeps.
+  __device__ __noinline__ int nth_tie(const Cut cut, const float t, const int r) const {
+    int* ties = reinterpret_cast<int*>(sh.list);
+    tm.sync();
+    if (tm.tid == 0) sh.n_list = 0;
+    tm.sync();
+    for_each([&](float x, int place) {
+      if (x == t && cut.keeps(x, place)) {
+        const int i = atomicAdd(&sh.n_list, 1);
+        if (i < sh.kList) ties[i] = place;
+      }
+    });
+    tm.sync();
+    const int n = sh.n_list;
+    if (n <= sh.kList) {
+      for (int i = tm.tid; i < n; i += NT) {
+        int front = 0;
+        for (int j = 0; j < n; ++j) front += ties[j] < ties[i];
+        if (front == r - 1) sh.place = ties[i];
+      }
+      tm.sync();
+      return sh.place;
+    }
+    int lo = 0, hi = row.n - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      int up_to = 0;
+      for_each([&](float x, int place) { up_to += x == t && place <= mid && cut.keeps(x, place); });
+      if (tm.sum(up_to) >= r) hi = mid; else lo = mid + 1;
+    }
+    return lo;
+  }
+
+  // A step with more values than the list takes: histograms of equal steps of the ordered bits, until they fit or are all the
+  // same (`copies` of one list entry).
+  template <bool MASS>
+  __device__ __noinline__ void narrow_keys(const Cut cut, const int k, const float p, const int b, const float scale, const float whole,
+                                           float& above, int& n_above, int& len, int& copies) const {
+    uint32_t key_lo = 0xffffffffu, key_hi = 0u;
+    for_each([&](float x, int place) {
+      if (cut.keeps(x, place) && bucket_of(x) == b) { const uint32_t key = ordered_key(x); key_lo = min(key_lo, key); key_hi = max(key_hi, key); }
+    });
+    key_lo = tm.reduce(key_lo, [](uint32_t a, uint32_t d) { return min(a, d); });
+    key_hi = tm.reduce(key_hi, [](uint32_t a, uint32_t d) { return max(a, d); });
+    int n = sh.n_list;
+    while (n > sh.kList && key_lo < key_hi) {
+      const int shift = max(0, 24 - __clz(key_hi - key_lo));
+      tm.sync();
+      clear_hist(tm, sh);
+      tm.sync();
+      for_each([&](float x, int place) {
+        const uint32_t key = ordered_key(x);
+        if (key >= key_lo && key <= key_hi && cut.keeps(x, place)) atomicAdd(&sh.hist[(key_hi - key) >> shift], MASS ? __float2uint_rn(weight(x) * scale) : 1u);
+      });
+      tm.sync();
+      uint32_t want = (uint32_t)(k - n_above);
+      if (MASS) {
+        uint32_t all = 0;
+        for (int i = tm.tid; i < kSampleBuckets; i += NT) all += sh.hist[i];
+        all = tm.reduce(all, [](uint32_t a, uint32_t d) { return a + d; });
+        want = min((uint32_t)fminf(fmaxf((p * whole - above) * scale, 1.f), 4294967040.f), max(1u, all));
+      }
+      find_bucket(tm, sh, want);
+      const int at = max(0, sh.bucket);
+      key_hi -= (uint32_t)at << shift;
+      key_lo = max(key_lo, key_hi - ((1u << shift) - 1u));
+      float more = 0.f;
+      int inside = 0, over = 0;
+      for_each([&](float x, int place) {
+        if (!cut.keeps(x, place)) return;
+        const uint32_t key = ordered_key(x);
+        if (key > key_hi) { over += 1; if (MASS) more += weight(x); }
+        else if (key >= key_lo) inside += 1;
+      });
+      n = tm.sum(inside);
+      n_above = tm.sum(over);
+      if (MASS) above = tm.sum(more);
+    }
+    tm.sync();
+    if (tm.tid == 0) sh.n_list = 0;
+    tm.sync();
+    const bool one = key_lo == key_hi;
+    for_each([&](float x, int place) {
+      const uint32_t key = ordered_key(x);
+      if (key < key_lo || key > key_hi || !cut.keeps(x, place)) return;
+      const int i = one ? 0 : atomicAdd(&sh.n_list, 1);
+      if (i < sh.kList) sh.list[i] = x;
+    });
+    tm.sync();
+    copies = one ? n : 1;
+    len = one ? min(n, 1) : n;
+  }
+
+  // narrow<true>'s decision by sums in 64 bits: first within the list that 32 bits found, then, should the border lie outside it,
+  // by bisection over all values.  Sets sh.found_*.
+  __device__ __noinline__ void narrow64(const Cut cut, const float p, const int len, const int copies) const {
+    float top = -INFINITY;
+    for (int j = 0; j < len; ++j) top = fmaxf(top, sh.list[j]);
+    double whole = 0., above = 0.;
+    for_each([&](float x, int place) {
+      if (!cut.keeps(x, place)) return;
+      const double w = weight64(x);
+      whole += w;
+      if (x > top) above += w;
+    });
+    whole = tm.sum(whole);
+    if (whole_row > 0.f) whole += rest.weight64(tm, m, inv_t);
+    above = tm.sum(above);
+    const double goal = (double)p * whole;
+    auto settle = [&](float x, double front, int same) {
+      note(x, min(same, max(1, (int)fmin(ceil((goal - front) / weight64(x)), 2147483647.))), same);
+    };
+    for (int i = tm.tid; i < len; i += NT) {
+      const float x = sh.list[i];
+      double front = above;
+      int same = 0;
+      for (int j = 0; j < len; ++j) {
+        const float y = sh.list[j];
+        if (y > x) front += weight64(y);
+        same += y == x;
+      }
+      same *= copies;
+      if ((front < goal || (front == 0. && goal <= 0.)) && front + weight64(x) * same >= goal) settle(x, front, same);
+    }
+    tm.sync();
+    if (sh.found != 0) return;
+    // greatest key whose weights and those of all greater ones reach the goal
+    uint32_t lo = kKeyNegInf + 1u, hi = ordered_key(m);
+    while (lo < hi) {
+      const uint32_t mid = lo + ((hi - lo + 1u) >> 1);
+      double reach = 0.;
+      for_each([&](float x, int place) { if (ordered_key(x) >= mid && cut.keeps(x, place)) reach += weight64(x); });
+      if (tm.sum(reach) >= goal) lo = mid; else hi = mid - 1u;
+    }
+    double front = 0.;
+    int same = 0;
+    float least = INFINITY;                                // the kept value at `lo`, or the least kept where rounding reaches none
+    for_each([&](float x, int place) {
+      if (!cut.keeps(x, place)) return;
+      const uint32_t key = ordered_key(x);
+      if (key > lo) front += weight64(x);
+      same += key == lo;
+      if (key >= lo) least = fminf(least, x);
+    });
+    front = tm.sum(front);
+    same = tm.sum(same);
+    least = tm.reduce(least, [](float a, float d) { return fminf(a, d); });
+    if (tm.tid == 0) {
+      if (same > 0) settle(least, front, same);
+      else note(least, 1, 1);
+    }
+    tm.sync();
+  }
+
+  template <class F>
+  __device__ __forceinline__ F kept_weight(const Cut cut, int i) const {
+    const float x = row.at(i);
+    return cut.keeps(x, i) ? (sizeof(F) == 8 ? (F)weight64(x) : (F)weight(x)) : F(0);
+  }
+  // The table of sums of the kept weights by groups, and the threads' sums (four groups each) up to and with their own; returns
+  // the whole.
+  template <class F>
+  __device__ __forceinline__ F tabulate(const Cut cut, F* table) const {
+    tm.sync();
+    F s = F(0);
+    for (int e = 0; e < 4; ++e) {
+      F t = F(0);
+      const int i0 = (4 * tm.tid + e) * group;
+      for (int i = i0; i < min(i0 + group, row.n); ++i) t += kept_weight<F>(cut, i);
+      table[4 * tm.tid + e] = t;
+      s += t;
+    }
+    s = tm.scan(s);
+    reinterpret_cast<F*>(sh.prefix)[tm.tid] = s;
+    tm.sync();
+    return reinterpret_cast<const F*>(sh.prefix)[NT - 1];
+  }
+
+  // Place of the first kept element at which the running sum exceeds u * whole; `sure` unless a border is within `slack`.
+  template <class F>
+  __device__ __forceinline__ int pick(const Cut cut, const F* table, F whole, float u, F slack, bool& sure) const {
+    const F* prefix = reinterpret_cast<const F*>(sh.prefix);
+    const F goal = (F)u * whole;
+    int lo = 0, hi = NT - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (prefix[mid] > goal) hi = mid; else lo = mid + 1;
+    }
+    F run = lo > 0 ? prefix[lo - 1] : F(0);
+    sure = false;
+    int last = -1;
+    // group by group from there on: rounding may leave the border just behind the thread's four
+    for (int e = 4 * lo; e < 4 * NT; ++e) {
+      const F s = table[e];
+      if (run + s <= goal && e + 1 < 4 * NT && (e + 1) * group < row.n) { run += s; continue; }
+      for (int i = e * group; i < min((e + 1) * group, row.n); ++i) {
+        const F w = kept_weight<F>(cut, i);
+        if (w > F(0)) {
+          last = i;
+          if (run + w > goal) { sure = goal - run > slack && run + w - goal > slack; return i; }
+        }
+        run += w;
+      }
+    }
+    // u next to 1: the last kept element with a weight
+    for (int i = row.n - 1; i >= 0 && last < 0; --i)
+      if (kept_weight<F>(cut, i) > F(0)) last = i;
+    return last;
+  }
+  // The same by a whole warp for one draw (all lanes return it): the lanes take a group's elements at once.
+  __device__ __forceinline__ int pick_together(const Cut cut, const float* table, float whole, float u, float slack, bool& sure) const {
+    const float* prefix = reinterpret_cast<const float*>(sh.prefix);
+    const int lane = tm.tid & 31;
+    const float goal = u * whole;
+    int lo = 0;
+    if (NW == 1) {
+      const uint32_t over = __ballot_sync(kFullMask, prefix[lane] > goal);
+      lo = over != 0u ? __ffs(over) - 1 : 31;
+    } else {
+      int hi = NT - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (prefix[mid] > goal) hi = mid; else lo = mid + 1;
+      }
+    }
+    float run = lo > 0 ? prefix[lo - 1] : 0.f;
+    const float4 t = reinterpret_cast<const float4*>(table)[lo];
+    int e = 4 * lo;
+    if (run + t.x <= goal) { run += t.x; ++e; if (run + t.y <= goal) { run += t.y; ++e; if (run + t.z <= goal) { run += t.z; ++e; } } }
+    sure = false;
+    for (int i0 = e * group; i0 < min((e + 1) * group, row.n); i0 += 32) {
+      const int i = i0 + lane;
+      const float w = i < min((e + 1) * group, row.n) ? kept_weight<float>(cut, i) : 0.f;
+      float upto = w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const float v = __shfl_up_sync(kFullMask, upto, o);
+        if (lane >= o) upto += v;
+      }
+      upto += run;
+      const uint32_t over = __ballot_sync(kFullMask, w > 0.f && upto > goal);
+      if (over != 0u) {
+        const int at = __ffs(over) - 1;
+        const float after = __shfl_sync(kFullMask, upto, at), own = __shfl_sync(kFullMask, w, at);
+        sure = goal - (after - own) > slack && after - goal > slack;
+        return i0 + at;
+      }
+      run = __shfl_sync(kFullMask, upto, 31);
+    }
+    return 0;                                              // not sure: 64 bits decide
+  }
+};
+
+// What a row's draws need besides its elements.
+struct RowLimits {
+  float temperature, top_p, min_p;
+  int top_k;
+};
+__device__ __forceinline__ RowLimits row_limits(const SampleParams& p, int64_t r) {
+  const int b = (int)(r / p.M);
+  RowLimits l;
+  l.temperature = p.temperature != nullptr ? __ldg(p.temperature + b) : 1.f;
+  l.top_k = p.top_k != nullptr ? __ldg(p.top_k + b) : 0;
+  l.top_p = p.top_p != nullptr ? __ldg(p.top_p + b) : 1.f;
+  l.min_p = p.min_p != nullptr ? __ldg(p.min_p + b) : 0.f;
+  return l;
+}
+struct Scale {                   // of the weights
+  double t64, inv_t;
+  float c;
+  __device__ __forceinline__ explicit Scale(float temperature) {
+    t64 = fmin((double)temperature, 1e30);
+    inv_t = 1. / t64;
+    c = (float)fmin(1.4426950408889634 * inv_t, 1e38);
+  }
+};
+// w >= min_p as a bound on x, rounded up to the next fp32.
+__device__ __forceinline__ float min_p_bound(float m, float min_p, double t64) {
+  return min_p < 1.f ? fminf(m, __double2float_ru((double)m + t64 * log((double)min_p))) : m;
+}
+template <bool BF16>
+__device__ __forceinline__ void store_draw(const SampleParams& p, int64_t r, int d, int token, float logq) {
+  const int64_t at = r * p.draws + d;
+  p.out_token[at] = token;
+  if (p.out_parent != nullptr) p.out_parent[at] = (int)(r % p.M);
+  float score = -INFINITY;
+  if (logq != -INFINITY) {
+    const float x = logit_at<BF16>(reinterpret_cast<const char*>(p.logits) + r * p.ld * (BF16 ? 2 : 4), token);
+    score = (p.row_score != nullptr ? __ldg(p.row_score + r) : 0.f) + (x - (p.row_lse != nullptr ? __ldg(p.row_lse + r) : 0.f));
+  }
+  p.out_score[at] = score;
+  if (p.out_logq != nullptr) p.out_logq[at] = logq;
+}
+template <int NW, bool BF16>
+__device__ __forceinline__ void store_all(const SampleParams& p, const Team<NW>& tm, int64_t r, int token, float logq) {
+  for (int d = tm.tid; d < p.draws; d += NW * 32) store_draw<BF16>(p, r, d, token, logq);
+}
+
+// The limits exactly, on a row that holds all elements they can keep, and the draws.  m: the largest value (finite).
+template <int NW, bool BF16, class Row>
+__device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row& row, const Team<NW>& tm, SampleShared<NW>& sh, int64_t r, float m,
+                                               const RowLimits& l, const Scale& sc, float whole_row, const LeftOut<BF16>& rest) {
+  constexpr int NT = NW * 32;
+  const Sampler<NW, Row, LeftOut<BF16>> s{row, tm, sh, m, sc.c, sc.inv_t, p.V > 2048 ? 0x1p-17f : 0x1p-18f, (row.n + 4 * NT - 1) / (4 * NT), whole_row, rest};
+  Cut cut = {-INFINITY, -1};
+  if (l.top_k > 0 && l.top_k < row.n) cut = s.template narrow<false>(cut, l.top_k, 0.f);
+  if (l.top_p < 1.f) cut = s.template narrow<true>(cut, 0, fmaxf(l.top_p, 0.f));
+  if (l.min_p > 0.f) {
+    const float least = min_p_bound(m, l.min_p, sc.t64);
+    if (least > cut.t) cut = Cut{least, 0x7fffffff};
+  }
+  float* table32 = reinterpret_cast<float*>(sh.table);
+  const float whole = s.template tabulate<float>(cut, table32);
+  const float log_whole = logf(whole);
+  auto number = [&](int d) {
+    const float u = __ldg(p.u + r * p.draws + d);
+    return u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
+  };
+  auto store = [&](int d, int place) {
+    place = max(place, 0);
+    store_draw<BF16>(p, r, d, row.token(place), (float)(((double)row.at(place) - (double)m) * sc.inv_t) - log_whole);
+  };
+  bool have64 = false;
+  double whole64 = 0.;
+  // few draws: a warp together for one after the other; many: each thread its own
+  const bool together = p.draws <= 8;
+  for (int d0 = 0; d0 < p.draws; d0 += together ? 1 : NT) {
+    const int d = d0 + (together ? 0 : tm.tid);
+    const bool in = d < p.draws && (!together || tm.tid < 32);
+    const float u = d < p.draws ? number(d) : 0.5f;
+    bool sure = false;
+    int place = -1;
+    if (!have64 && in) {
+      place = together ? s.pick_together(cut, table32, whole, u, s.margin * whole, sure)
+                       : s.template pick<float>(cut, table32, whole, u, s.margin * whole, sure);
+    }
+    const int doubt = tm.reduce(in && !sure ? 1 : 0, [](int a, int e) { return a | e; });
+    if (doubt) {
+      if (!have64) {
+        whole64 = s.template tabulate<double>(cut, sh.table);
+        have64 = true;
+      }
+      bool ignored;
+      if (in && !sure && (!together || tm.tid == 0)) place = s.template pick<double>(cut, sh.table, whole64, u, 0., ignored);
+    }
+    if (in && (!together || tm.tid == 0)) store(d, place);
+  }
+}
+
+// A row without a list yet: dense, or with more allowed tokens than a list takes.  SHARED (one warp): the row lies in the list's
+// place and is narrowed there; otherwise every pass reads it.
+template <int NW, bool BF16, bool SHARED>
+__device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF16> row, const Team<NW>& tm, SampleShared<NW>& sh, float* vals,
+                                             uint16_t* tokens, int64_t r, int n, const RowLimits& l) {
+  constexpr int NT = NW * 32;
+  const int lane = tm.tid & 31, warp = tm.tid >> 5;
+  // a warp's quads are neighbours, lane by lane: `iters` of 32
+  const int quads = (p.V + 3) >> 2, iters = (quads + NT - 1) / NT, first = warp * 32 * iters + lane;
+  float4* const shared = reinterpret_cast<float4*>(vals);
+  auto none = []() { return make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY); };
+  auto quad = [&](int q) { return q < quads ? (SHARED ? shared[q] : row.quad(q)) : none(); };
+  float m = -INFINITY;
+  for (int i0 = 0; i0 < iters; i0 += 8) {                  // eight loads in flight
+    float4 t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = i0 + i < iters && first + 32 * (i0 + i) < quads ? row.quad(first + 32 * (i0 + i)) : none();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      m = max_nan(m, max_nan(max_nan(t[i].x, t[i].y), max_nan(t[i].z, t[i].w)));
+      if (SHARED && i0 + i < iters && first + 32 * (i0 + i) < quads) shared[first + 32 * (i0 + i)] = t[i];
+    }
+  }
+  m = tm.reduce(m, [](float a, float b) { return max_nan(a, b); });
+  if (!(m > -INFINITY)) {                                  // nothing, or NaN
+    if (m != m && tm.tid == 0) flag_status(p.d_status, GRACE_DEV_NAN);
+    store_all<NW, BF16>(p, tm, r, 0, -INFINITY);
+    return;
+  }
+  // (A thread writes and reads the same quads up to the list, so nothing waits here.)
+  if (m == INFINITY) {
+    row.inf = true;
+    m = 0.f;
+    if (SHARED) {
+      for (int i = 0; i < iters; ++i) {
+        const int q = first + 32 * i;
+        if (q < quads) { const float4 t = shared[q]; shared[q] = make_float4(row.shown(t.x), row.shown(t.y), row.shown(t.z), row.shown(t.w)); }
+      }
+    }
+  }
+  if (!(l.temperature > 0.f)) {
+    int at = 0x7fffffff;
+    for (int i = 0; i < iters; ++i) {
+      const int q = first + 32 * i;
+      const float4 t = quad(q);
+      const int j = t.x == m ? 0 : t.y == m ? 1 : t.z == m ? 2 : t.w == m ? 3 : 4;
+      if (j < 4) at = min(at, 4 * q + j);
+    }
+    at = tm.reduce(at, [](int a, int b) { return min(a, b); });
+    store_all<NW, BF16>(p, tm, r, at, 0.f);
+    return;
+  }
+  const Scale sc(l.temperature);
+  // a bound below which nothing is kept (and nothing counts: top-p's sum is that of the top_k, whatever min-p leaves of them)
+  const bool by_count = l.top_k > 0 && l.top_k < n, by_mass = !by_count && l.top_p < 1.f;
+  float bound = l.min_p > 0.f && !(by_count && l.top_p < 1.f) ? min_p_bound(m, l.min_p, sc.t64) : -INFINITY;
+  float whole_row = 0.f;
+  if (by_count) {
+    clear_hist(tm, sh);
+    tm.sync();
+    const float cs = sc.c * kSampleSteps;
+    auto count = [&](float x) {
+      if (x > -INFINITY) atomicAdd(&sh.hist[min(kSampleBuckets - 1, (int)((m - x) * cs))], 1u);
+    };
+    for (int i = 0; i < iters; ++i) {
+      const float4 t = quad(first + 32 * i);
+      count(t.x); count(t.y); count(t.z); count(t.w);
+    }
+    tm.sync();
+    find_bucket(tm, sh, (uint32_t)l.top_k);
+    const int b = sh.bucket;
+    // the step's far edge, further by what rounding can make of it
+    if (b >= 0 && b < kSampleBuckets - 1) bound = fmaxf(bound, m - ((float)(b + 1) * 1.0001f) / cs - fabsf(m) * 0x1p-20f);
+  } else if (by_mass) {
+    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+    for (int i = 0; i < iters; ++i) {
+      const float4 t = quad(first + 32 * i);
+      s0 += sample_ex2((t.x - m) * sc.c); s1 += sample_ex2((t.y - m) * sc.c);
+      s2 += sample_ex2((t.z - m) * sc.c); s3 += sample_ex2((t.w - m) * sc.c);
+    }
+    whole_row = tm.sum((s0 + s1) + (s2 + s3));
+    const float light = (1.f - fmaxf(l.top_p, 0.f)) * whole_row / (float)n * 0.999f;
+    bound = fmaxf(bound, m + log2f(light) / sc.c - 1e-4f / sc.c - fabsf(m) * 0x1p-20f);
+  }
+  const bool limited = by_count || by_mass || l.min_p > 0.f;
+  if (!limited && p.V <= p.cap) {
+    if (!SHARED) {
+      for (int i = 0; i < iters; ++i)
+        if (first + 32 * i < quads) shared[first + 32 * i] = quad(first + 32 * i);
+    }
+    tm.sync();
+    const RowShared all{vals, nullptr, p.V};
+    limit_and_draw<NW, BF16>(p, all, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f});
+    return;
+  }
+  if (limited) {
+    bound = fmaxf(fminf(bound, m), -3.402823466e38f);      // (-inf is in no list)
+    int before = 0;                                        // elements of the list in front of this warp's
+    if (NW > 1) {
+      int mine = 0;
+      for (int i = 0; i < iters; ++i) {
+        const float4 t = quad(first + 32 * i);
+        mine += (int)(t.x >= bound) + (int)(t.y >= bound) + (int)(t.z >= bound) + (int)(t.w >= bound);
+      }
+      const int upto = tm.scan(mine);
+      int* starts = reinterpret_cast<int*>(sh.hist);       // (free by now)
+      tm.sync();
+      if (lane == 31) starts[warp] = upto;
+      tm.sync();
+      before = warp > 0 ? starts[warp - 1] : 0;
+    }
+    // Four quads at a time: counts in the bytes of a word, summed over the lanes at once.  In place (SHARED, one warp) the list
+    // never reaches the quads that are still to be read.
+    for (int i0 = 0; i0 < iters; i0 += 4) {
+      float4 t[4];
+      uint32_t counts = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        t[i] = i0 + i < iters ? quad(first + 32 * (i0 + i)) : none();
+        counts += ((uint32_t)(t[i].x >= bound) + (uint32_t)(t[i].y >= bound) + (uint32_t)(t[i].z >= bound) + (uint32_t)(t[i].w >= bound)) << (8 * i);
+      }
+      uint32_t upto = counts;                              // at most 128 a byte
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t v = __shfl_up_sync(kFullMask, upto, o);
+        if (lane >= o) upto += v;
+      }
+      const uint32_t all = __shfl_sync(kFullMask, upto, 31), own = upto - counts;
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        int at = before + (int)((own >> (8 * i)) & 255u);
+        const int token = 4 * (first + 32 * (i0 + i));
+        auto take = [&](float x, int j) {
+          if (x >= bound) {
+            if (SHARED || at < p.cap) { vals[at] = x; tokens[at] = (uint16_t)(token + j); }
+            ++at;
+          }
+        };
+        take(t[i].x, 0); take(t[i].y, 1); take(t[i].z, 2); take(t[i].w, 3);
+        before += (int)((all >> (8 * i)) & 255u);
+      }
+      __syncwarp();
+    }
+    const int kept = NW == 1 ? before : tm.reduce(before, [](int a, int b) { return max(a, b); });
+    tm.sync();
+    if (SHARED || kept <= p.cap) {
+      const RowShared list{vals, tokens, kept};
+      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, sc, whole_row, LeftOut<BF16>{row, bound});
+      return;
+    }
+  }
+  if constexpr (!SHARED) limit_and_draw<NW, BF16>(p, row, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f});
+}
+
+// LISTS: with allow bits.
+template <int NW, bool BF16, bool LISTS, bool SHARED>
+__global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32)
+sample_kernel(const SampleParams p) {
+  pdl_wait();
+  pdl_trigger();
+  extern __shared__ __align__(16) uint8_t smem[];
+  constexpr int NT = NW * 32, kTeams = NW == 1 ? 4 : 1;
+  const int team = NW == 1 ? threadIdx.x >> 5 : 0;
+  const int64_t r = (int64_t)blockIdx.x * kTeams + team;
+  if (r >= p.R) return;                                    // whole teams
+  SampleShared<NW>& sh = *reinterpret_cast<SampleShared<NW>*>(smem + (size_t)team * p.team_bytes);
+  float* vals = reinterpret_cast<float*>(&sh + 1);
+  uint16_t* tokens = reinterpret_cast<uint16_t*>(vals + p.cap);
+  const Team<NW> tm{NW == 1 ? (int)(threadIdx.x & 31) : (int)threadIdx.x, sh.red};
+  const RowLimits l = row_limits(p, r);
+  const int words = (p.V + 63) >> 6;
+  const uint64_t* allow = LISTS ? p.allow + r * words : nullptr;
+  const RowGlobal<BF16> row{reinterpret_cast<const char*>(p.logits) + r * p.ld * (BF16 ? 2 : 4), allow, p.V, p.vec, false};
+  int n = p.V;
+  if constexpr (LISTS) {
+    // the allowed tokens' places: a thread's words are neighbours, so that the list is in order
+    const int per = (words + NT - 1) / NT;
+    auto word = [&](int i) {
+      const int w = tm.tid * per + i;
+      uint64_t a = i < per && w < words ? __ldg(allow + w) : 0ull;
+      if (w == words - 1 && (p.V & 63)) a &= (1ull << (p.V & 63)) - 1ull;
+      return a;
+    };
+    const uint64_t a0 = word(0);
+    int count = __popcll(a0);
+    for (int i = 1; i < per; ++i) count += __popcll(word(i));
+    const int upto = tm.scan(count);
+    n = NW == 1 ? __shfl_sync(kFullMask, upto, 31) : tm.reduce(upto, [](int a, int b) { return max(a, b); });
+    if (n <= p.cap) {
+      int at = upto - count;
+      for (int i = 0; i < per; ++i) {
+        const uint64_t a = i == 0 ? a0 : word(i);
+        const int token0 = (tm.tid * per + i) * 64;
+        for (uint32_t h = (uint32_t)a; h != 0u; h &= h - 1u) tokens[at++] = (uint16_t)(token0 + __ffs((int)h) - 1);
+        for (uint32_t h = (uint32_t)(a >> 32); h != 0u; h &= h - 1u) tokens[at++] = (uint16_t)(token0 + 31 + __ffs((int)h));
+      }
+      tm.sync();
+      float m = -INFINITY;
+      for (int i0 = 0; i0 < n; i0 += 4 * NT) {             // four loads in flight
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = i0 + i * NT + tm.tid;
+          x[i] = j < n ? logit_at<BF16>(row.row, tokens[j]) : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int j = i0 + i * NT + tm.tid;
+          if (j < n) vals[j] = x[i];
+          m = max_nan(m, x[i]);
+        }
+      }
+      m = tm.reduce(m, [](float a, float b) { return max_nan(a, b); });
+      tm.sync();
+      if (!(m > -INFINITY)) {                              // nothing, or NaN
+        if (m != m && tm.tid == 0) flag_status(p.d_status, GRACE_DEV_NAN);
+        store_all<NW, BF16>(p, tm, r, 0, -INFINITY);
+        return;
+      }
+      if (m == INFINITY) {                                 // those at +inf weigh 1 each, all others nothing
+        for (int i = tm.tid; i < n; i += NT) vals[i] = vals[i] == INFINITY ? 0.f : -INFINITY;
+        tm.sync();
+        m = 0.f;
+      }
+      if (!(l.temperature > 0.f)) {
+        int first = 0x7fffffff;
+        for (int i = tm.tid; i < n; i += NT)
+          if (vals[i] == m) first = min(first, i);
+        first = tm.reduce(first, [](int a, int b) { return min(a, b); });
+        store_all<NW, BF16>(p, tm, r, tokens[first], 0.f);
+        return;
+      }
+      const RowShared list{vals, tokens, n};
+      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, Scale(l.temperature), 0.f, LeftOut<BF16>{row, 0.f});
+      return;
+    }
+  }
+  sample_dense<NW, BF16, SHARED>(p, row, tm, sh, vals, tokens, r, n, l);
+}
+
+template <int NW, bool BF16, bool LISTS>
+static grace_status_t launch_sample(SampleParams p, cudaStream_t s) {
+  // A row of up to 16384 tokens fits its list; without a constraint a warp's row lies in the list's place from the start
+  // (SHARED).  Under one the list takes half the tokens: a row with more is read again by every pass, as are longer rows.
+  constexpr bool kShared = NW == 1 && !LISTS;
+  constexpr int kTeams = NW == 1 ? 4 : 1;
+  const int row = (p.V + 15) & ~15, half = ((p.V + 31) / 2 + 15) & ~15;
+  p.cap = NW == 32 ? 16384 : (LISTS && row > 512 ? half : row);
+  p.team_bytes = (int)sizeof(SampleShared<NW>) + p.cap * 6;
+  static_assert(sizeof(SampleShared<NW>) % 16 == 0 && sizeof(SampleShared<32>) + 16384 * 6 <= 227 * 1024, "");
+  p.team_bytes = (p.team_bytes + 15) & ~15;
+  static unsigned long long attr_set_devices = 0;
+  DeviceSetup su(&attr_set_devices);
+  if (su) {
+    GRACE_CUDA_TRY(cudaFuncSetAttribute(sample_kernel<NW, BF16, LISTS, kShared>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
+    su.done();
+  }
+  GRACE_CUDA_TRY(launch_pdl(sample_kernel<NW, BF16, LISTS, kShared>, dim3((unsigned)((p.R + kTeams - 1) / kTeams)), dim3(NW == 1 ? 128 : NW * 32),
+                            (size_t)p.team_bytes * kTeams, s, p));
+  GRACE_LAUNCH_CHECK();
+  return GRACE_OK;
+}
+template <bool BF16>
+static grace_status_t run_sample(const SampleParams& p, cudaStream_t s) {
+  // Warps of a row: one per 2048 tokens at least, more while the GPU is not filled by the rows (a pass over a row is then as
+  // long as its threads' part).
+  const bool lists = p.allow != nullptr;
+  if (p.V > 16384) return lists ? launch_sample<32, BF16, true>(p, s) : launch_sample<32, BF16, false>(p, s);
+  if (p.V > 8192 || (p.V > 1024 && p.R <= kSms)) return lists ? launch_sample<8, BF16, true>(p, s) : launch_sample<8, BF16, false>(p, s);
+  if (p.V > 2048 || (p.V > 256 && p.R <= 4 * kSms)) return lists ? launch_sample<4, BF16, true>(p, s) : launch_sample<4, BF16, false>(p, s);
+  return lists ? launch_sample<1, BF16, true>(p, s) : launch_sample<1, BF16, false>(p, s);
+}
+
+}  // namespace grace
