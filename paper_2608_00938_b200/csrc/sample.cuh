@@ -34,7 +34,7 @@ struct SampleParams {
   int32_t* d_status;
   int64_t ld, R;
   int M, V, draws, vec;          // vec: quads of a row lie on their own size
-  int cap;                       // elements that a row's list takes, a multiple of 16
+  int cap, tokens_cap;           // elements in a team's shared memory, of a list with tokens (multiples of 16)
   int team_bytes;                // shared memory of a team
 };
 
@@ -48,6 +48,8 @@ __device__ __forceinline__ float sample_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// A weight in 64 bits, for the rows that need them (a function of its own: e^ in 64 bits is long).
+static __device__ __noinline__ double sample_weight64(float x, float m, double inv_t) { return exp(((double)x - (double)m) * inv_t); }
 // The larger of two values, NaN if either is.
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
@@ -165,11 +167,11 @@ struct LeftOut {
   RowGlobal<BF16> row;
   float bound;
   template <int NW>
-  __device__ __noinline__ double weight64(const Team<NW>& tm, float m, double inv_t) const {
+  __device__ __forceinline__ double weight64(const Team<NW> tm, float m, double inv_t) const {
     double t = 0.;
     for (int i = tm.tid; i < row.n; i += NW * 32) {
       const float x = row.at(i);
-      if (x > -INFINITY && x < bound) t += exp(((double)x - (double)m) * inv_t);
+      if (x > -INFINITY && x < bound) t += sample_weight64(x, m, inv_t);
     }
     return tm.sum(t);
   }
@@ -181,19 +183,25 @@ struct Cut {
   __device__ __forceinline__ bool keeps(float x, int place) const { return x > t || (x == t && place <= last); }
 };
 
-// A team's shared memory, in front of its list (vals [cap], tokens [cap]).
+// A team's shared memory, in front of its elements (vals [cap], tokens [tokens_cap]).
 template <int NW>
 struct SampleShared {
   static constexpr int kList = NW == 1 ? 64 : 256;         // values of a histogram step that are resolved one by one
-  double table[NW * 128];                                  // sums of weights over groups of elements, four groups a thread
-  double prefix[NW * 32];
+  union {
+    double table[NW * 128];                                // sums of weights over groups of elements, four groups a thread
+    uint32_t hist[kSampleBuckets];
+  };
+  union {
+    double prefix[NW * 32];
+    float list[kList];
+  };
   double red[NW < 2 ? 2 : NW];
-  uint32_t hist[kSampleBuckets];
-  float list[kList];
   int n_list, bucket, found, found_r;
   float found_t;
   uint32_t above;
   int found_all, place;
+  float above_w;
+  int len, copies, pad[1];
 };
 
 // First step at which the histogram's running sum reaches `target` (sh.bucket) and the sum in front of it (sh.above);
@@ -233,12 +241,13 @@ __device__ __forceinline__ void clear_hist(const Team<NW>& tm, SampleShared<NW>&
   for (int i = tm.tid; i < kSampleBuckets / 4; i += NW * 32) reinterpret_cast<uint4*>(sh.hist)[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// The exact work on a row (a list, as a rule).
+// The exact work on a row (a list, as a rule).  Its steps are functions of their own where they are long, and take it by value:
+// an object whose address they had would lie in memory, and every loop would read its members from there.
 template <int NW, class Row, class Rest>
 struct Sampler {
-  const Row& row;
-  const Team<NW>& tm;
-  SampleShared<NW>& sh;
+  Row row;
+  Team<NW> tm;
+  SampleShared<NW>* shared;
   float m;                       // largest value
   float c;                       // log2(e) / T
   double inv_t;                  // 1 / T
@@ -246,46 +255,49 @@ struct Sampler {
   int group;                     // elements of a table entry
   // top-p counts elements that the list leaves out: their weight with the list's (0: the row is all there is), and where they are
   float whole_row;
-  const Rest& rest;
+  Rest rest;
   static constexpr int NT = NW * 32;
+  static constexpr int kList = SampleShared<NW>::kList;
 
   __device__ __forceinline__ float weight(float x) const { return sample_ex2((x - m) * c); }
-  __device__ __forceinline__ double weight64(float x) const { return exp(((double)x - (double)m) * inv_t); }
+  __device__ __forceinline__ double weight64(float x) const { return sample_weight64(x, m, inv_t); }
   __device__ __forceinline__ int bucket_of(float x) const { return min(kSampleBuckets - 1, (int)((m - x) * c * kSampleSteps)); }
   template <class F>
   __device__ __forceinline__ void for_each(F f) const {
     for (int i = tm.tid; i < row.n; i += NT) f(row.at(i), i);
   }
   __device__ __forceinline__ void note(float t, int r, int same) const {
-    sh.found_t = t; sh.found_r = r; sh.found_all = r == same; sh.found = 1;
+    shared->found_t = t; shared->found_r = r; shared->found_all = r == same; shared->found = 1;
   }
 
   // Narrows `cut` to its first k elements (MASS false), or to the fewest whose weights reach p of the sum of its weights.
   template <bool MASS>
-  __device__ __noinline__ Cut narrow(const Cut cut, const int k, const float p) const {
+  static __device__ __noinline__ Cut narrow(const Sampler s, const Cut cut, const int k, const float p) { return s.template narrow_<MASS>(cut, k, p); }
+  template <bool MASS>
+  __device__ __forceinline__ Cut narrow_(const Cut cut, const int k, const float p) const {
     // fixed point: the sum of any row below 2^32
     const float scale = MASS ? exp2f(31.f - ceilf(log2f((float)row.n))) : 1.f;
     auto share = [&](float x) { return MASS ? __float2uint_rn(weight(x) * scale) : 1u; };
     tm.sync();
-    clear_hist(tm, sh);
-    if (tm.tid == 0) { sh.n_list = 0; sh.found = 0; }
+    clear_hist(tm, *shared);
+    if (tm.tid == 0) { shared->n_list = 0; shared->found = 0; }
     tm.sync();
     for_each([&](float x, int place) {
-      if (cut.keeps(x, place)) atomicAdd(&sh.hist[bucket_of(x)], share(x));
+      if (cut.keeps(x, place)) atomicAdd(&shared->hist[bucket_of(x)], share(x));
     });
     tm.sync();
     auto mass_goal = [&](float want) {                     // within what the histogram holds
       uint32_t all = 0;
-      for (int i = tm.tid; i < kSampleBuckets; i += NT) all += sh.hist[i];
+      for (int i = tm.tid; i < kSampleBuckets; i += NT) all += shared->hist[i];
       all = tm.reduce(all, [](uint32_t a, uint32_t b) { return a + b; });
       if (want < 0.f) want = (float)all * p;
       return min(max(1u, (uint32_t)fminf(want, 4294967040.f)), max(1u, all));
     };
-    find_bucket(tm, sh, MASS ? mass_goal(whole_row > 0.f ? whole_row * scale * p : -1.f) : (uint32_t)k);
-    if (sh.bucket < 0) return cut;                         // no more than k elements
-    const int b = sh.bucket;
+    find_bucket(tm, *shared, MASS ? mass_goal(whole_row > 0.f ? whole_row * scale * p : -1.f) : (uint32_t)k);
+    if (shared->bucket < 0) return cut;                         // no more than k elements
+    const int b = shared->bucket;
     float whole = 0.f, above = 0.f;
-    int n_above = (int)sh.above;
+    int n_above = (int)shared->above;
     for_each([&](float x, int place) {
       if (!cut.keeps(x, place)) return;
       const int at = bucket_of(x);
@@ -295,8 +307,8 @@ struct Sampler {
         above += at < b ? w : 0.f;
       }
       if (at == b) {
-        const int i = atomicAdd(&sh.n_list, 1);
-        if (i < sh.kList) sh.list[i] = x;
+        const int i = atomicAdd(&shared->n_list, 1);
+        if (i < kList) shared->list[i] = x;
       }
     });
     if (MASS) {
@@ -304,17 +316,23 @@ struct Sampler {
       above = tm.sum(above);
     }
     tm.sync();
-    const int n = sh.n_list;
+    const int n = shared->n_list;
     int len = n, copies = 1;
-    if (n > sh.kList) narrow_keys<MASS>(cut, k, p, b, scale, whole, above, n_above, len, copies);
+    if (n > kList) {
+      narrow_keys<MASS>(*this, cut, k, p, b, scale, whole, above, n_above);
+      above = shared->above_w;
+      n_above = (int)shared->above;
+      len = shared->len;
+      copies = shared->copies;
+    }
     // The list resolved: the value at which the count or the sum of weights in front passes the goal.
     for (int i = tm.tid; i < len; i += NT) {
-      const float x = sh.list[i];
+      const float x = shared->list[i];
       int same = 0;
       if (MASS) {
         float front = above;
         for (int j = 0; j < len; ++j) {
-          const float y = sh.list[j];
+          const float y = shared->list[j];
           if (y > x) front += weight(y);
           same += y == x;
         }
@@ -326,44 +344,45 @@ struct Sampler {
         }
       } else {
         int front = n_above;
-        for (int j = 0; j < len; ++j) { const float y = sh.list[j]; front += y > x; same += y == x; }
+        for (int j = 0; j < len; ++j) { const float y = shared->list[j]; front += y > x; same += y == x; }
         same *= copies;
         if (front < k && k <= front + same) note(x, k - front, same);
       }
     }
     tm.sync();
-    if (MASS && sh.found == 0) narrow64(cut, p, len, copies);
-    Cut out = {sh.found_t, 0x7fffffff};
-    if (sh.found_all != 0) {
+    if (MASS && shared->found == 0) narrow64(*this, cut, p, len, copies);
+    Cut out = {shared->found_t, 0x7fffffff};
+    if (shared->found_all != 0) {
       if (out.t == cut.t) out.last = cut.last;
       return out;
     }
-    out.last = nth_tie(cut, out.t, sh.found_r);
+    out.last = nth_tie(*this, cut, out.t, shared->found_r);
     return out;
   }
 
   // Place of the r-th of the elements with value t that `cut` keeps.
-  __device__ __noinline__ int nth_tie(const Cut cut, const float t, const int r) const {
-    int* ties = reinterpret_cast<int*>(sh.list);
+  static __device__ __noinline__ int nth_tie(const Sampler s, const Cut cut, const float t, const int r) { return s.nth_tie_(cut, t, r); }
+  __device__ __forceinline__ int nth_tie_(const Cut cut, const float t, const int r) const {
+    int* ties = reinterpret_cast<int*>(shared->list);
     tm.sync();
-    if (tm.tid == 0) sh.n_list = 0;
+    if (tm.tid == 0) shared->n_list = 0;
     tm.sync();
     for_each([&](float x, int place) {
       if (x == t && cut.keeps(x, place)) {
-        const int i = atomicAdd(&sh.n_list, 1);
-        if (i < sh.kList) ties[i] = place;
+        const int i = atomicAdd(&shared->n_list, 1);
+        if (i < kList) ties[i] = place;
       }
     });
     tm.sync();
-    const int n = sh.n_list;
-    if (n <= sh.kList) {
+    const int n = shared->n_list;
+    if (n <= kList) {
       for (int i = tm.tid; i < n; i += NT) {
         int front = 0;
         for (int j = 0; j < n; ++j) front += ties[j] < ties[i];
-        if (front == r - 1) sh.place = ties[i];
+        if (front == r - 1) shared->place = ties[i];
       }
       tm.sync();
-      return sh.place;
+      return shared->place;
     }
     int lo = 0, hi = row.n - 1;
     while (lo < hi) {
@@ -378,34 +397,39 @@ struct Sampler {
   // A step with more values than the list takes: histograms of equal steps of the ordered bits, until they fit or are all the
   // same (`copies` of one list entry).
   template <bool MASS>
-  __device__ __noinline__ void narrow_keys(const Cut cut, const int k, const float p, const int b, const float scale, const float whole,
-                                           float& above, int& n_above, int& len, int& copies) const {
+  static __device__ __noinline__ void narrow_keys(const Sampler s, const Cut cut, const int k, const float p, const int b, const float scale, const float whole,
+                                                  const float above, const int n_above) {
+    s.template narrow_keys_<MASS>(cut, k, p, b, scale, whole, above, n_above);
+  }
+  template <bool MASS>
+  __device__ __forceinline__ void narrow_keys_(const Cut cut, const int k, const float p, const int b, const float scale, const float whole,
+                                               float above, int n_above) const {
     uint32_t key_lo = 0xffffffffu, key_hi = 0u;
     for_each([&](float x, int place) {
       if (cut.keeps(x, place) && bucket_of(x) == b) { const uint32_t key = ordered_key(x); key_lo = min(key_lo, key); key_hi = max(key_hi, key); }
     });
     key_lo = tm.reduce(key_lo, [](uint32_t a, uint32_t d) { return min(a, d); });
     key_hi = tm.reduce(key_hi, [](uint32_t a, uint32_t d) { return max(a, d); });
-    int n = sh.n_list;
-    while (n > sh.kList && key_lo < key_hi) {
+    int n = shared->n_list;
+    while (n > kList && key_lo < key_hi) {
       const int shift = max(0, 24 - __clz(key_hi - key_lo));
       tm.sync();
-      clear_hist(tm, sh);
+      clear_hist(tm, *shared);
       tm.sync();
       for_each([&](float x, int place) {
         const uint32_t key = ordered_key(x);
-        if (key >= key_lo && key <= key_hi && cut.keeps(x, place)) atomicAdd(&sh.hist[(key_hi - key) >> shift], MASS ? __float2uint_rn(weight(x) * scale) : 1u);
+        if (key >= key_lo && key <= key_hi && cut.keeps(x, place)) atomicAdd(&shared->hist[(key_hi - key) >> shift], MASS ? __float2uint_rn(weight(x) * scale) : 1u);
       });
       tm.sync();
       uint32_t want = (uint32_t)(k - n_above);
       if (MASS) {
         uint32_t all = 0;
-        for (int i = tm.tid; i < kSampleBuckets; i += NT) all += sh.hist[i];
+        for (int i = tm.tid; i < kSampleBuckets; i += NT) all += shared->hist[i];
         all = tm.reduce(all, [](uint32_t a, uint32_t d) { return a + d; });
         want = min((uint32_t)fminf(fmaxf((p * whole - above) * scale, 1.f), 4294967040.f), max(1u, all));
       }
-      find_bucket(tm, sh, want);
-      const int at = max(0, sh.bucket);
+      find_bucket(tm, *shared, want);
+      const int at = max(0, shared->bucket);
       key_hi -= (uint32_t)at << shift;
       key_lo = max(key_lo, key_hi - ((1u << shift) - 1u));
       float more = 0.f;
@@ -421,25 +445,30 @@ struct Sampler {
       if (MASS) above = tm.sum(more);
     }
     tm.sync();
-    if (tm.tid == 0) sh.n_list = 0;
+    if (tm.tid == 0) shared->n_list = 0;
     tm.sync();
     const bool one = key_lo == key_hi;
     for_each([&](float x, int place) {
       const uint32_t key = ordered_key(x);
       if (key < key_lo || key > key_hi || !cut.keeps(x, place)) return;
-      const int i = one ? 0 : atomicAdd(&sh.n_list, 1);
-      if (i < sh.kList) sh.list[i] = x;
+      const int i = one ? 0 : atomicAdd(&shared->n_list, 1);
+      if (i < kList) shared->list[i] = x;
     });
+    if (tm.tid == 0) {
+      shared->above_w = above;
+      shared->above = (uint32_t)n_above;
+      shared->copies = one ? n : 1;
+      shared->len = one ? min(n, 1) : n;
+    }
     tm.sync();
-    copies = one ? n : 1;
-    len = one ? min(n, 1) : n;
   }
 
   // narrow<true>'s decision by sums in 64 bits: first within the list that 32 bits found, then, should the border lie outside it,
-  // by bisection over all values.  Sets sh.found_*.
-  __device__ __noinline__ void narrow64(const Cut cut, const float p, const int len, const int copies) const {
+  // by bisection over all values.  Sets shared->found_*.
+  static __device__ __noinline__ void narrow64(const Sampler s, const Cut cut, const float p, const int len, const int copies) { s.narrow64_(cut, p, len, copies); }
+  __device__ __forceinline__ void narrow64_(const Cut cut, const float p, const int len, const int copies) const {
     float top = -INFINITY;
-    for (int j = 0; j < len; ++j) top = fmaxf(top, sh.list[j]);
+    for (int j = 0; j < len; ++j) top = fmaxf(top, shared->list[j]);
     double whole = 0., above = 0.;
     for_each([&](float x, int place) {
       if (!cut.keeps(x, place)) return;
@@ -455,11 +484,11 @@ struct Sampler {
       note(x, min(same, max(1, (int)fmin(ceil((goal - front) / weight64(x)), 2147483647.))), same);
     };
     for (int i = tm.tid; i < len; i += NT) {
-      const float x = sh.list[i];
+      const float x = shared->list[i];
       double front = above;
       int same = 0;
       for (int j = 0; j < len; ++j) {
-        const float y = sh.list[j];
+        const float y = shared->list[j];
         if (y > x) front += weight64(y);
         same += y == x;
       }
@@ -467,7 +496,7 @@ struct Sampler {
       if ((front < goal || (front == 0. && goal <= 0.)) && front + weight64(x) * same >= goal) settle(x, front, same);
     }
     tm.sync();
-    if (sh.found != 0) return;
+    if (shared->found != 0) return;
     // greatest key whose weights and those of all greater ones reach the goal
     uint32_t lo = kKeyNegInf + 1u, hi = ordered_key(m);
     while (lo < hi) {
@@ -510,20 +539,25 @@ struct Sampler {
     for (int e = 0; e < 4; ++e) {
       F t = F(0);
       const int i0 = (4 * tm.tid + e) * group;
-      for (int i = i0; i < min(i0 + group, row.n); ++i) t += kept_weight<F>(cut, i);
+      // each thread from another of its elements on, round once: side by side they would all be on one bank
+      int k = tm.tid % group;
+      for (int i = 0; i < group; ++i) {
+        if (i0 + k < row.n) t += kept_weight<F>(cut, i0 + k);
+        k = k + 1 == group ? 0 : k + 1;
+      }
       table[4 * tm.tid + e] = t;
       s += t;
     }
     s = tm.scan(s);
-    reinterpret_cast<F*>(sh.prefix)[tm.tid] = s;
+    reinterpret_cast<F*>(shared->prefix)[tm.tid] = s;
     tm.sync();
-    return reinterpret_cast<const F*>(sh.prefix)[NT - 1];
+    return reinterpret_cast<const F*>(shared->prefix)[NT - 1];
   }
 
   // Place of the first kept element at which the running sum exceeds u * whole; `sure` unless a border is within `slack`.
   template <class F>
   __device__ __forceinline__ int pick(const Cut cut, const F* table, F whole, float u, F slack, bool& sure) const {
-    const F* prefix = reinterpret_cast<const F*>(sh.prefix);
+    const F* prefix = reinterpret_cast<const F*>(shared->prefix);
     const F goal = (F)u * whole;
     int lo = 0, hi = NT - 1;
     while (lo < hi) {
@@ -551,9 +585,15 @@ struct Sampler {
       if (kept_weight<F>(cut, i) > F(0)) last = i;
     return last;
   }
+  // A draw by sums in 64 bits, for the threads that are not sure (`mine`); `build`: the table does not hold them yet.
+  static __device__ __noinline__ int place64(const Sampler s, const Cut cut, const float u, const bool mine, const bool build, const int place) {
+    const double whole = build ? s.template tabulate<double>(cut, s.shared->table) : s.shared->prefix[NT - 1];
+    bool ignored;
+    return mine ? s.template pick<double>(cut, s.shared->table, whole, u, 0., ignored) : place;
+  }
   // The same by a whole warp for one draw (all lanes return it): the lanes take a group's elements at once.
   __device__ __forceinline__ int pick_together(const Cut cut, const float* table, float whole, float u, float slack, bool& sure) const {
-    const float* prefix = reinterpret_cast<const float*>(sh.prefix);
+    const float* prefix = reinterpret_cast<const float*>(shared->prefix);
     const int lane = tm.tid & 31;
     const float goal = u * whole;
     int lo = 0;
@@ -595,18 +635,22 @@ struct Sampler {
   }
 };
 
-// What a row's draws need besides its elements.
+// What a row's draws need besides its elements: read before them, so that no trip to memory waits for another.
 struct RowLimits {
   float temperature, top_p, min_p;
   int top_k;
+  float score, lse, u;           // u: this thread's first draw
 };
-__device__ __forceinline__ RowLimits row_limits(const SampleParams& p, int64_t r) {
+__device__ __forceinline__ RowLimits row_limits(const SampleParams& p, int64_t r, int tid) {
   const int b = (int)(r / p.M);
   RowLimits l;
   l.temperature = p.temperature != nullptr ? __ldg(p.temperature + b) : 1.f;
   l.top_k = p.top_k != nullptr ? __ldg(p.top_k + b) : 0;
   l.top_p = p.top_p != nullptr ? __ldg(p.top_p + b) : 1.f;
   l.min_p = p.min_p != nullptr ? __ldg(p.min_p + b) : 0.f;
+  l.score = p.row_score != nullptr ? __ldg(p.row_score + r) : 0.f;
+  l.lse = p.row_lse != nullptr ? __ldg(p.row_lse + r) : 0.f;
+  l.u = tid < p.draws ? __ldg(p.u + r * p.draws + tid) : 0.f;
   return l;
 }
 struct Scale {                   // of the weights
@@ -622,33 +666,29 @@ struct Scale {                   // of the weights
 __device__ __forceinline__ float min_p_bound(float m, float min_p, double t64) {
   return min_p < 1.f ? fminf(m, __double2float_ru((double)m + t64 * log((double)min_p))) : m;
 }
-template <bool BF16>
-__device__ __forceinline__ void store_draw(const SampleParams& p, int64_t r, int d, int token, float logq) {
+// x: the token's logit
+__device__ __forceinline__ void store_draw(const SampleParams& p, const RowLimits& l, int64_t r, int d, int token, float x, float logq) {
   const int64_t at = r * p.draws + d;
   p.out_token[at] = token;
   if (p.out_parent != nullptr) p.out_parent[at] = (int)(r % p.M);
-  float score = -INFINITY;
-  if (logq != -INFINITY) {
-    const float x = logit_at<BF16>(reinterpret_cast<const char*>(p.logits) + r * p.ld * (BF16 ? 2 : 4), token);
-    score = (p.row_score != nullptr ? __ldg(p.row_score + r) : 0.f) + (x - (p.row_lse != nullptr ? __ldg(p.row_lse + r) : 0.f));
-  }
-  p.out_score[at] = score;
+  p.out_score[at] = logq == -INFINITY ? -INFINITY : l.score + (x - l.lse);
   if (p.out_logq != nullptr) p.out_logq[at] = logq;
 }
-template <int NW, bool BF16>
-__device__ __forceinline__ void store_all(const SampleParams& p, const Team<NW>& tm, int64_t r, int token, float logq) {
-  for (int d = tm.tid; d < p.draws; d += NW * 32) store_draw<BF16>(p, r, d, token, logq);
+template <int NW>
+__device__ __forceinline__ void store_all(const SampleParams& p, const RowLimits& l, const Team<NW>& tm, int64_t r, int token, float x, float logq) {
+  for (int d = tm.tid; d < p.draws; d += NW * 32) store_draw(p, l, r, d, token, x, logq);
 }
 
 // The limits exactly, on a row that holds all elements they can keep, and the draws.  m: the largest value (finite).
 template <int NW, bool BF16, class Row>
 __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row& row, const Team<NW>& tm, SampleShared<NW>& sh, int64_t r, float m,
-                                               const RowLimits& l, const Scale& sc, float whole_row, const LeftOut<BF16>& rest) {
+                                               const RowLimits& l, const Scale& sc, float whole_row, const LeftOut<BF16>& rest, bool infinite) {
   constexpr int NT = NW * 32;
-  const Sampler<NW, Row, LeftOut<BF16>> s{row, tm, sh, m, sc.c, sc.inv_t, p.V > 2048 ? 0x1p-17f : 0x1p-18f, (row.n + 4 * NT - 1) / (4 * NT), whole_row, rest};
+  using S = Sampler<NW, Row, LeftOut<BF16>>;
+  const S s{row, tm, &sh, m, sc.c, sc.inv_t, p.V > 2048 ? 0x1p-17f : 0x1p-18f, (row.n + 4 * NT - 1) / (4 * NT), whole_row, rest};
   Cut cut = {-INFINITY, -1};
-  if (l.top_k > 0 && l.top_k < row.n) cut = s.template narrow<false>(cut, l.top_k, 0.f);
-  if (l.top_p < 1.f) cut = s.template narrow<true>(cut, 0, fmaxf(l.top_p, 0.f));
+  if (l.top_k > 0 && l.top_k < row.n) cut = S::template narrow<false>(s, cut, l.top_k, 0.f);
+  if (l.top_p < 1.f) cut = S::template narrow<true>(s, cut, 0, fmaxf(l.top_p, 0.f));
   if (l.min_p > 0.f) {
     const float least = min_p_bound(m, l.min_p, sc.t64);
     if (least > cut.t) cut = Cut{least, 0x7fffffff};
@@ -656,22 +696,19 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
   float* table32 = reinterpret_cast<float*>(sh.table);
   const float whole = s.template tabulate<float>(cut, table32);
   const float log_whole = logf(whole);
-  auto number = [&](int d) {
-    const float u = __ldg(p.u + r * p.draws + d);
-    return u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-  };
   auto store = [&](int d, int place) {
     place = max(place, 0);
-    store_draw<BF16>(p, r, d, row.token(place), (float)(((double)row.at(place) - (double)m) * sc.inv_t) - log_whole);
+    const float x = row.at(place);
+    store_draw(p, l, r, d, row.token(place), infinite ? INFINITY : x, (float)(((double)x - (double)m) * sc.inv_t) - log_whole);
   };
   bool have64 = false;
-  double whole64 = 0.;
   // few draws: a warp together for one after the other; many: each thread its own
   const bool together = p.draws <= 8;
   for (int d0 = 0; d0 < p.draws; d0 += together ? 1 : NT) {
     const int d = d0 + (together ? 0 : tm.tid);
     const bool in = d < p.draws && (!together || tm.tid < 32);
-    const float u = d < p.draws ? number(d) : 0.5f;
+    float u = together ? __shfl_sync(kFullMask, l.u, d) : (d0 == 0 ? l.u : (in ? __ldg(p.u + r * p.draws + d) : 0.f));
+    u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
     bool sure = false;
     int place = -1;
     if (!have64 && in) {
@@ -680,12 +717,8 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
     }
     const int doubt = tm.reduce(in && !sure ? 1 : 0, [](int a, int e) { return a | e; });
     if (doubt) {
-      if (!have64) {
-        whole64 = s.template tabulate<double>(cut, sh.table);
-        have64 = true;
-      }
-      bool ignored;
-      if (in && !sure && (!together || tm.tid == 0)) place = s.template pick<double>(cut, sh.table, whole64, u, 0., ignored);
+      place = S::place64(s, cut, u, in && !sure && (!together || tm.tid == 0), !have64, place);
+      have64 = true;
     }
     if (in && (!together || tm.tid == 0)) store(d, place);
   }
@@ -704,20 +737,36 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   auto none = []() { return make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY); };
   auto quad = [&](int q) { return q < quads ? (SHARED ? shared[q] : row.quad(q)) : none(); };
   float m = -INFINITY;
-  for (int i0 = 0; i0 < iters; i0 += 8) {                  // eight loads in flight
-    float4 t[8];
+  auto see = [&](const float4& t) { m = max_nan(m, max_nan(max_nan(t.x, t.y), max_nan(t.z, t.w))); };
+  int i0 = 0;
+  if (row.allow == nullptr && p.vec) {                     // eight loads in flight, of whole quads
+    const int whole = min(iters, (p.V / 4 - first + 31) / 32);
+    for (; i0 + 8 <= whole; i0 += 8) {
+      float4 t[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = i0 + i < iters && first + 32 * (i0 + i) < quads ? row.quad(first + 32 * (i0 + i)) : none();
+      for (int i = 0; i < 8; ++i) t[i] = row.whole_quad(first + 32 * (i0 + i));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      m = max_nan(m, max_nan(max_nan(t[i].x, t[i].y), max_nan(t[i].z, t[i].w)));
+      for (int i = 0; i < 8; ++i) {
+        see(t[i]);
+        if (SHARED) shared[first + 32 * (i0 + i)] = t[i];
+      }
+    }
+  }
+#pragma unroll 1
+  for (; i0 < iters; i0 += 4) {
+    float4 t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = i0 + i < iters && first + 32 * (i0 + i) < quads ? row.quad(first + 32 * (i0 + i)) : none();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      see(t[i]);
       if (SHARED && i0 + i < iters && first + 32 * (i0 + i) < quads) shared[first + 32 * (i0 + i)] = t[i];
     }
   }
   m = tm.reduce(m, [](float a, float b) { return max_nan(a, b); });
   if (!(m > -INFINITY)) {                                  // nothing, or NaN
     if (m != m && tm.tid == 0) flag_status(p.d_status, GRACE_DEV_NAN);
-    store_all<NW, BF16>(p, tm, r, 0, -INFINITY);
+    store_all<NW>(p, l, tm, r, 0, 0.f, -INFINITY);
     return;
   }
   // (A thread writes and reads the same quads up to the list, so nothing waits here.)
@@ -740,7 +789,7 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
       if (j < 4) at = min(at, 4 * q + j);
     }
     at = tm.reduce(at, [](int a, int b) { return min(a, b); });
-    store_all<NW, BF16>(p, tm, r, at, 0.f);
+    store_all<NW>(p, l, tm, r, at, row.inf ? INFINITY : m, 0.f);
     return;
   }
   const Scale sc(l.temperature);
@@ -775,93 +824,99 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
     const float light = (1.f - fmaxf(l.top_p, 0.f)) * whole_row / (float)n * 0.999f;
     bound = fmaxf(bound, m + log2f(light) / sc.c - 1e-4f / sc.c - fabsf(m) * 0x1p-20f);
   }
-  const bool limited = by_count || by_mass || l.min_p > 0.f;
-  if (!limited && p.V <= p.cap) {
-    if (!SHARED) {
-      for (int i = 0; i < iters; ++i)
-        if (first + 32 * i < quads) shared[first + 32 * i] = quad(first + 32 * i);
-    }
-    tm.sync();
-    const RowShared all{vals, nullptr, p.V};
-    limit_and_draw<NW, BF16>(p, all, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f});
-    return;
-  }
-  if (limited) {
+  if (by_count || by_mass || l.min_p > 0.f) {
     bound = fmaxf(fminf(bound, m), -3.402823466e38f);      // (-inf is in no list)
-    int before = 0;                                        // elements of the list in front of this warp's
-    if (NW > 1) {
-      int mine = 0;
-      for (int i = 0; i < iters; ++i) {
-        const float4 t = quad(first + 32 * i);
-        mine += (int)(t.x >= bound) + (int)(t.y >= bound) + (int)(t.z >= bound) + (int)(t.w >= bound);
+    // Four quads at a time: counts in the bytes of a word, summed over the lanes at once.
+    static_assert(kSampleMostV <= 4 * 32 * 32 * 16, "");   // at most 16 quads a thread
+    uint32_t counts[4] = {0, 0, 0, 0};
+    int mine = 0;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      if (4 * g >= iters) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float4 t = 4 * g + i < iters ? quad(first + 32 * (4 * g + i)) : none();
+        counts[g] += ((uint32_t)(t.x >= bound) + (uint32_t)(t.y >= bound) + (uint32_t)(t.z >= bound) + (uint32_t)(t.w >= bound)) << (8 * i);
       }
+      mine += (int)((counts[g] * 0x01010101u) >> 24);      // the four bytes' sum: at most 16
+    }
+    int before = 0, kept;                                  // elements of the list in front of this warp's, and in all
+    if (NW == 1) {
+      kept = __reduce_add_sync(kFullMask, mine);
+    } else {
       const int upto = tm.scan(mine);
       int* starts = reinterpret_cast<int*>(sh.hist);       // (free by now)
       tm.sync();
       if (lane == 31) starts[warp] = upto;
       tm.sync();
       before = warp > 0 ? starts[warp - 1] : 0;
+      kept = starts[NW - 1];
     }
-    // Four quads at a time: counts in the bytes of a word, summed over the lanes at once.  In place (SHARED, one warp) the list
-    // never reaches the quads that are still to be read.
-    for (int i0 = 0; i0 < iters; i0 += 4) {
-      float4 t[4];
-      uint32_t counts = 0;
+    if (kept <= p.tokens_cap) {
+      // In place (SHARED, one warp) the list never reaches the quads that are still to be read.
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        t[i] = i0 + i < iters ? quad(first + 32 * (i0 + i)) : none();
-        counts += ((uint32_t)(t[i].x >= bound) + (uint32_t)(t[i].y >= bound) + (uint32_t)(t[i].z >= bound) + (uint32_t)(t[i].w >= bound)) << (8 * i);
-      }
-      uint32_t upto = counts;                              // at most 128 a byte
+      for (int g = 0; g < 4; ++g) {
+        if (4 * g >= iters) break;
+        uint32_t upto = counts[g];                         // at most 128 a byte
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const uint32_t v = __shfl_up_sync(kFullMask, upto, o);
-        if (lane >= o) upto += v;
-      }
-      const uint32_t all = __shfl_sync(kFullMask, upto, 31), own = upto - counts;
-      __syncwarp();
+        for (int o = 1; o < 32; o <<= 1) {
+          const uint32_t v = __shfl_up_sync(kFullMask, upto, o);
+          if (lane >= o) upto += v;
+        }
+        const uint32_t all = __shfl_sync(kFullMask, upto, 31), own = upto - counts[g];
+        float4 t[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        int at = before + (int)((own >> (8 * i)) & 255u);
-        const int token = 4 * (first + 32 * (i0 + i));
-        auto take = [&](float x, int j) {
-          if (x >= bound) {
-            if (SHARED || at < p.cap) { vals[at] = x; tokens[at] = (uint16_t)(token + j); }
-            ++at;
-          }
-        };
-        take(t[i].x, 0); take(t[i].y, 1); take(t[i].z, 2); take(t[i].w, 3);
-        before += (int)((all >> (8 * i)) & 255u);
+        for (int i = 0; i < 4; ++i) t[i] = 4 * g + i < iters ? quad(first + 32 * (4 * g + i)) : none();
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          int at = before + (int)((own >> (8 * i)) & 255u);
+          const int token = 4 * (first + 32 * (4 * g + i));
+          auto take = [&](float x, int j) {
+            if (x >= bound) { vals[at] = x; tokens[at] = (uint16_t)(token + j); ++at; }
+          };
+          take(t[i].x, 0); take(t[i].y, 1); take(t[i].z, 2); take(t[i].w, 3);
+          before += (int)((all >> (8 * i)) & 255u);
+        }
+        __syncwarp();
       }
-      __syncwarp();
-    }
-    const int kept = NW == 1 ? before : tm.reduce(before, [](int a, int b) { return max(a, b); });
-    tm.sync();
-    if (SHARED || kept <= p.cap) {
+      tm.sync();
       const RowShared list{vals, tokens, kept};
-      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, sc, whole_row, LeftOut<BF16>{row, bound});
+      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, sc, whole_row, LeftOut<BF16>{row, bound}, row.inf);
       return;
     }
   }
-  if constexpr (!SHARED) limit_and_draw<NW, BF16>(p, row, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f});
+  // no limit, or one that leaves more than a list takes: the whole row
+  if (p.V <= p.cap) {
+    if (!SHARED) {
+      for (int i = 0; i < iters; ++i)
+        if (first + 32 * i < quads) shared[first + 32 * i] = quad(first + 32 * i);
+    }
+    tm.sync();
+    const RowShared all{vals, nullptr, p.V};
+    limit_and_draw<NW, BF16>(p, all, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f}, row.inf);
+  } else if constexpr (!SHARED) {
+    limit_and_draw<NW, BF16>(p, row, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f}, row.inf);
+  }
 }
 
 // LISTS: with allow bits.
 template <int NW, bool BF16, bool LISTS, bool SHARED>
-__global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32)
+__global__ void __launch_bounds__(NW == 1 ? 64 : NW * 32, NW == 1 ? 16 : (NW == 32 ? 1 : 24 / NW))
 sample_kernel(const SampleParams p) {
   pdl_wait();
   pdl_trigger();
   extern __shared__ __align__(16) uint8_t smem[];
-  constexpr int NT = NW * 32, kTeams = NW == 1 ? 4 : 1;
+  constexpr int NT = NW * 32, kTeams = NW == 1 ? 2 : 1;
   const int team = NW == 1 ? threadIdx.x >> 5 : 0;
   const int64_t r = (int64_t)blockIdx.x * kTeams + team;
   if (r >= p.R) return;                                    // whole teams
   SampleShared<NW>& sh = *reinterpret_cast<SampleShared<NW>*>(smem + (size_t)team * p.team_bytes);
   float* vals = reinterpret_cast<float*>(&sh + 1);
   uint16_t* tokens = reinterpret_cast<uint16_t*>(vals + p.cap);
+  static_assert(sizeof(SampleShared<NW>) % 16 == 0, "");
   const Team<NW> tm{NW == 1 ? (int)(threadIdx.x & 31) : (int)threadIdx.x, sh.red};
-  const RowLimits l = row_limits(p, r);
+  const RowLimits l = row_limits(p, r, tm.tid);
   const int words = (p.V + 63) >> 6;
   const uint64_t* allow = LISTS ? p.allow + r * words : nullptr;
   const RowGlobal<BF16> row{reinterpret_cast<const char*>(p.logits) + r * p.ld * (BF16 ? 2 : 4), allow, p.V, p.vec, false};
@@ -880,7 +935,7 @@ sample_kernel(const SampleParams p) {
     for (int i = 1; i < per; ++i) count += __popcll(word(i));
     const int upto = tm.scan(count);
     n = NW == 1 ? __shfl_sync(kFullMask, upto, 31) : tm.reduce(upto, [](int a, int b) { return max(a, b); });
-    if (n <= p.cap) {
+    if (n <= p.tokens_cap) {
       int at = upto - count;
       for (int i = 0; i < per; ++i) {
         const uint64_t a = i == 0 ? a0 : word(i);
@@ -908,10 +963,11 @@ sample_kernel(const SampleParams p) {
       tm.sync();
       if (!(m > -INFINITY)) {                              // nothing, or NaN
         if (m != m && tm.tid == 0) flag_status(p.d_status, GRACE_DEV_NAN);
-        store_all<NW, BF16>(p, tm, r, 0, -INFINITY);
+        store_all<NW>(p, l, tm, r, 0, 0.f, -INFINITY);
         return;
       }
-      if (m == INFINITY) {                                 // those at +inf weigh 1 each, all others nothing
+      const bool infinite = m == INFINITY;
+      if (infinite) {                                      // those at +inf weigh 1 each, all others nothing
         for (int i = tm.tid; i < n; i += NT) vals[i] = vals[i] == INFINITY ? 0.f : -INFINITY;
         tm.sync();
         m = 0.f;
@@ -921,11 +977,11 @@ sample_kernel(const SampleParams p) {
         for (int i = tm.tid; i < n; i += NT)
           if (vals[i] == m) first = min(first, i);
         first = tm.reduce(first, [](int a, int b) { return min(a, b); });
-        store_all<NW, BF16>(p, tm, r, tokens[first], 0.f);
+        store_all<NW>(p, l, tm, r, tokens[first], infinite ? INFINITY : m, 0.f);
         return;
       }
       const RowShared list{vals, tokens, n};
-      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, Scale(l.temperature), 0.f, LeftOut<BF16>{row, 0.f});
+      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, Scale(l.temperature), 0.f, LeftOut<BF16>{row, 0.f}, infinite);
       return;
     }
   }
@@ -934,22 +990,23 @@ sample_kernel(const SampleParams p) {
 
 template <int NW, bool BF16, bool LISTS>
 static grace_status_t launch_sample(SampleParams p, cudaStream_t s) {
-  // A row of up to 16384 tokens fits its list; without a constraint a warp's row lies in the list's place from the start
-  // (SHARED).  Under one the list takes half the tokens: a row with more is read again by every pass, as are longer rows.
+  // Without a constraint a warp's row lies in shared memory from the start (SHARED); a longer one of up to 16384 tokens, read by
+  // every pass before, comes there when no list of half its tokens holds what can be kept.  Under a constraint there is room
+  // for half the tokens; a row with more allowed ones is read by every pass, as are longer rows.
   constexpr bool kShared = NW == 1 && !LISTS;
-  constexpr int kTeams = NW == 1 ? 4 : 1;
-  const int row = (p.V + 15) & ~15, half = ((p.V + 31) / 2 + 15) & ~15;
-  p.cap = NW == 32 ? 16384 : (LISTS && row > 512 ? half : row);
-  p.team_bytes = (int)sizeof(SampleShared<NW>) + p.cap * 6;
-  static_assert(sizeof(SampleShared<NW>) % 16 == 0 && sizeof(SampleShared<32>) + 16384 * 6 <= 227 * 1024, "");
-  p.team_bytes = (p.team_bytes + 15) & ~15;
+  constexpr int kTeams = NW == 1 ? 2 : 1;
+  const int row = (p.V + 15) & ~15, half = p.V <= 512 ? row : (p.V / 2 + 15) & ~15;
+  p.cap = NW == 32 ? 16384 : (LISTS ? half : row);
+  p.tokens_cap = NW == 32 ? 16384 : half;
+  p.team_bytes = ((int)sizeof(SampleShared<NW>) + p.cap * 4 + p.tokens_cap * 2 + 15) & ~15;
+  static_assert(sizeof(SampleShared<32>) + 16384 * 6 <= 227 * 1024, "");
   static unsigned long long attr_set_devices = 0;
   DeviceSetup su(&attr_set_devices);
   if (su) {
     GRACE_CUDA_TRY(cudaFuncSetAttribute(sample_kernel<NW, BF16, LISTS, kShared>, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024));
     su.done();
   }
-  GRACE_CUDA_TRY(launch_pdl(sample_kernel<NW, BF16, LISTS, kShared>, dim3((unsigned)((p.R + kTeams - 1) / kTeams)), dim3(NW == 1 ? 128 : NW * 32),
+  GRACE_CUDA_TRY(launch_pdl(sample_kernel<NW, BF16, LISTS, kShared>, dim3((unsigned)((p.R + kTeams - 1) / kTeams)), dim3(NW == 1 ? 64 : NW * 32),
                             (size_t)p.team_bytes * kTeams, s, p));
   GRACE_LAUNCH_CHECK();
   return GRACE_OK;
