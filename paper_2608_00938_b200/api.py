@@ -190,23 +190,38 @@ def _stream():
     return torch.cuda.current_stream().cuda_stream
 
 
-def _need(ok, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
+def _refuse(where: str, what: str):
+    raise ValueError(f"{where}: {what}")
 
 
-def _arg(t, where: str, name: str, dtype, shape=None, rows: bool = False):
-    """Device pointer of an optional tensor argument of the current device, checked: its type, its shape, and that it is
-    contiguous (rows: 2-D with contiguous rows)."""
+def _device() -> int:
     import torch
+    return torch.cuda.current_device()
+
+
+def _arg(t, where: str, name: str, dtype, device: int, shape=None):
+    """Device pointer of an optional tensor argument, checked: on the current device, its type, its shape, contiguous."""
     if t is None:
         return None
-    _need(t.is_cuda and t.get_device() == torch.cuda.current_device(), f"{where}: {name} is not on the current CUDA device")
-    _need(t.dtype == dtype, f"{where}: {name} is {t.dtype}, not {dtype}")
-    _need(shape is None or tuple(t.shape) == shape, f"{where}: {name} has shape {tuple(t.shape)}, not {shape}")
-    _need((t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1)) if rows else t.is_contiguous(),
-          f"{where}: {name} {'has no contiguous rows' if rows else 'is not contiguous'}")
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        _refuse(where, f"{name} is a {t.dtype} of {tuple(t.shape)} on {t.device}, not a contiguous {dtype}"
+                       f"{'' if shape is None else f' of {shape}'} on the current CUDA device")
     return t.data_ptr()
+
+
+def _rows(t, where: str, name: str, dtype, device: int, shape=None):
+    """(device pointer, row stride) of an optional 2-D tensor argument with contiguous rows, checked.  A single row may carry any
+    stride; it counts as its width then."""
+    if t is None:
+        return None, 0
+    if t.dtype is not dtype or t.get_device() != device or t.dim() != 2 or (shape is not None and t.shape != shape):
+        _refuse(where, f"{name} is a {t.dtype} of {tuple(t.shape)} on {t.device}, not a {dtype}"
+                       f"{'' if shape is None else f' of {shape}'} on the current CUDA device")
+    ld, one = t.stride()
+    rows, width = t.shape
+    if one != 1 and width != 1:
+        _refuse(where, f"{name} has no contiguous rows")
+    return t.data_ptr(), (ld if rows > 1 or ld > width else width)
 
 
 def version() -> int:
@@ -663,15 +678,11 @@ def grace_layer_norm(x, gamma, beta, out, eps: float = 1e-5):
     return out
 
 
-def _row_stride(t):
-    """Elements between rows; a single row may carry any stride, so it counts as its width."""
-    return t.stride(0) if t.shape[0] > 1 else max(t.shape[1], t.stride(0))
-
-
 def grace_quantize_rows_e4m3(w: np.ndarray):
     """Host: fp32 [N, K] -> (e4m3 bit patterns uint8 [N, K], scales fp32 [N]): the weights of grace_linear_act."""
     w = np.ascontiguousarray(w, dtype=np.float32)
-    _need(w.ndim == 2, "grace_quantize_rows_e4m3: w is not 2-D")
+    if w.ndim != 2:
+        _refuse("grace_quantize_rows_e4m3", "w is not 2-D")
     q, scale = np.empty(w.shape, np.uint8), np.empty(w.shape[0], np.float32)
     _check(_quantize_rows_e4m3(w.ctypes.data, w.shape[0], w.shape[1], q.ctypes.data, scale.ctypes.data),
            "grace_quantize_rows_e4m3")
@@ -684,22 +695,27 @@ def grace_rms_norm(x, gamma, out, eps: float = 1e-6, delta=None, x_out=None, sca
     x fp32 or bf16 [R, D]; delta bf16 [R, D] or None; x_out as x; out bf16, or float8_e4m3fn with scale fp32 [R] (one scale
     per row: the operand of grace_linear_act).  Rows may have any stride."""
     import torch
-    where = "grace_rms_norm"
-    _need(x.dim() == 2 and x.dtype in (torch.float32, torch.bfloat16), f"{where}: x is not fp32 or bf16 [R, D]")
-    shape = R, D = tuple(x.shape)
-    f32, e4m3 = x.dtype == torch.float32, out.dtype == torch.float8_e4m3fn
-    xp = _arg(x, where, "x", x.dtype, shape, True)
+    where, dev = "grace_rms_norm", _device()
+    kind = x.dtype
+    f32, e4m3 = kind is torch.float32, out.dtype is torch.float8_e4m3fn
+    if x.dim() != 2 or not (f32 or kind is torch.bfloat16):
+        _refuse(where, "x is not fp32 or bf16 [R, D]")
+    shape = x.shape
+    R, D = shape
     if delta is None:
-        _need(x_out is None, f"{where}: x_out without delta")
+        if x_out is not None:
+            _refuse(where, "x_out without delta")
     elif x_out is None:
         x_out = x
-    _need((scale is not None) == e4m3, f"{where}: scale belongs to an e4m3 out")
-    yp = _arg(out, where, "out", torch.float8_e4m3fn if e4m3 else torch.bfloat16, shape, True)
-    _check(_rms_norm(xp if f32 else None, None if f32 else xp, _row_stride(x), _arg(delta, where, "delta", torch.bfloat16, shape, True),
-                     0 if delta is None else _row_stride(delta), _arg(x_out, where, "x_out", x.dtype, shape, True),
-                     0 if x_out is None else _row_stride(x_out), _arg(gamma, where, "gamma", torch.float32, (D,)),
-                     None if e4m3 else yp, yp if e4m3 else None, _row_stride(out),
-                     _arg(scale, where, "scale", torch.float32, (R,)), R, D, eps, _stream()), where)
+    if (scale is not None) != e4m3:
+        _refuse(where, "scale belongs to an e4m3 out")
+    xp, ldx = _rows(x, where, "x", kind, dev)
+    dp, ldd = _rows(delta, where, "delta", torch.bfloat16, dev, shape)
+    op, ldo = (xp, ldx) if x_out is x else _rows(x_out, where, "x_out", kind, dev, shape)
+    yp, ldy = _rows(out, where, "out", torch.float8_e4m3fn if e4m3 else torch.bfloat16, dev, shape)
+    _check(_rms_norm(xp if f32 else None, None if f32 else xp, ldx, dp, ldd, op, ldo, _arg(gamma, where, "gamma", torch.float32, dev, (D,)),
+                     None if e4m3 else yp, yp if e4m3 else None, ldy, _arg(scale, where, "scale", torch.float32, dev, (R,)), R, D, eps,
+                     _stream()), where)
     return out
 
 
@@ -709,23 +725,29 @@ def grace_linear_act(x, w, y, bias=None, act: str = "none", residual=None, x_sca
     x [M, K], w [N, K]: both bf16 (no scales) or both float8_e4m3fn with x_scale fp32 [M], w_scale fp32 [N] (None: 1); bias fp32 [N];
     y [M, N] bf16 or fp32; residual as y (may be y).  act: none, relu, gelu, gelu_tanh, silu.  Rows may have any stride."""
     import torch
-    where = "grace_linear_act"
-    _need(act in ACTIVATIONS, f"{where}: no activation {act!r}")
-    _need(x.dim() == 2 and w.dim() == 2 and x.shape[1] == w.shape[1], f"{where}: x {tuple(x.shape)} and w {tuple(w.shape)} do not multiply")
+    where, dev = "grace_linear_act", _device()
+    number = ACTIVATIONS.get(act)
+    if number is None:
+        _refuse(where, f"no activation {act!r}")
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
+        _refuse(where, f"x {tuple(x.shape)} and w {tuple(w.shape)} do not multiply")
     (M, K), N = x.shape, w.shape[0]
-    f32, e4m3 = y.dtype == torch.float32, x.dtype == torch.float8_e4m3fn
-    kind = torch.float8_e4m3fn if e4m3 else torch.bfloat16
-    _need(e4m3 or (x_scale is None and w_scale is None), f"{where}: scales belong to e4m3 operands")
-    xp, wp = _arg(x, where, "x", kind, None, True), _arg(w, where, "w", kind, None, True)
-    yp = _arg(y, where, "y", torch.float32 if f32 else torch.bfloat16, (M, N), True)
-    rp, ldr = _arg(residual, where, "residual", y.dtype, (M, N), True), 0 if residual is None else _row_stride(residual)
-    rest = (_arg(bias, where, "bias", torch.float32, (N,)), ACTIVATIONS[act], rp, ldr, None if f32 else yp, yp if f32 else None, _row_stride(y),
-            M, N, K, _stream())
+    f32, e4m3 = y.dtype is torch.float32, x.dtype is torch.float8_e4m3fn
+    kind, shape = (torch.float8_e4m3fn if e4m3 else torch.bfloat16), (M, N)
+    xp, ldx = _rows(x, where, "x", kind, dev)
+    wp, ldw = _rows(w, where, "w", kind, dev)
+    yp, ldy = _rows(y, where, "y", torch.float32 if f32 else torch.bfloat16, dev, shape)
+    rp, ldr = (yp, ldy) if residual is y else _rows(residual, where, "residual", y.dtype, dev, shape)
+    bp = _arg(bias, where, "bias", torch.float32, dev, (N,))
+    yb, yf = (None, yp) if f32 else (yp, None)
     if e4m3:
-        _check(_linear_act_e4m3(xp, _row_stride(x), _arg(x_scale, where, "x_scale", torch.float32, (M,)), wp, _row_stride(w),
-                                _arg(w_scale, where, "w_scale", torch.float32, (N,)), *rest), where)
+        _check(_linear_act_e4m3(xp, ldx, _arg(x_scale, where, "x_scale", torch.float32, dev, (M,)), wp, ldw,
+                                _arg(w_scale, where, "w_scale", torch.float32, dev, (N,)), bp, number, rp, ldr, yb, yf, ldy, M, N, K,
+                                _stream()), where)
     else:
-        _check(_linear_act(xp, _row_stride(x), wp, _row_stride(w), *rest), where)
+        if x_scale is not None or w_scale is not None:
+            _refuse(where, "scales belong to e4m3 operands")
+        _check(_linear_act(xp, ldx, wp, ldw, bp, number, rp, ldr, yb, yf, ldy, M, N, K, _stream()), where)
     return y
 
 
@@ -736,22 +758,26 @@ def grace_sample(logits, u, out_score, out_token, B: int, M: int, allow_bits=Non
     allow_bits int64 [B*M, ceil(V/64)]; row_score, row_lse fp32 [B*M]; temperature, top_p, min_p fp32 [B], top_k int32 [B] (None: 1
     and no limit).  Outputs of B*M*draws elements each: out_score, out_logq fp32, out_token, out_parent int32."""
     import torch
-    where = "grace_sample"
-    _need(logits.dim() == 2 and logits.dtype in (torch.float32, torch.bfloat16), f"{where}: logits are not fp32 or bf16 [R, V]")
+    where, dev = "grace_sample", _device()
+    f32, i32, kind = torch.float32, torch.int32, logits.dtype
+    bf16 = kind is torch.bfloat16
+    if logits.dim() != 2 or u.dim() != 2 or logits.shape[0] != B * M or not (bf16 or kind is f32):
+        _refuse(where, f"logits are not fp32 or bf16 [{B} x {M}, V], or u is not 2-D")
     R, V = logits.shape
-    _need(R == B * M and u.dim() == 2, f"{where}: logits have {R} rows, not {B} x {M}, or u is not 2-D")
     draws = u.shape[1]
-    f32, i32, bf16 = torch.float32, torch.int32, logits.dtype == torch.bfloat16
-    lp = _arg(logits, where, "logits", logits.dtype, None, True)
+    lp, ld = _rows(logits, where, "logits", kind, dev)
+    n, rows, requests = R * draws, (R,), (B,)
     for name, t in (("out_score", out_score), ("out_token", out_token), ("out_logq", out_logq), ("out_parent", out_parent)):
-        _need(t is None or t.numel() == R * draws, f"{where}: {name} does not hold {R} x {draws} elements")
-    _check(_sample(None if bf16 else lp, lp if bf16 else None, _row_stride(logits),
-                   _arg(allow_bits, where, "allow_bits", torch.int64, (R, (V + 63) // 64)), _arg(row_score, where, "row_score", f32, (R,)),
-                   _arg(row_lse, where, "row_lse", f32, (R,)), _arg(temperature, where, "temperature", f32, (B,)),
-                   _arg(top_k, where, "top_k", i32, (B,)), _arg(top_p, where, "top_p", f32, (B,)), _arg(min_p, where, "min_p", f32, (B,)),
-                   _arg(u, where, "u", f32, (R, draws)), B, M, V, draws, _arg(out_score, where, "out_score", f32),
-                   _arg(out_logq, where, "out_logq", f32), _arg(out_parent, where, "out_parent", i32), _arg(out_token, where, "out_token", i32),
-                   _arg(d_status, where, "d_status", i32), _stream()), where)
+        if t is not None and t.numel() != n:
+            _refuse(where, f"{name} does not hold {R} x {draws} elements")
+    _check(_sample(None if bf16 else lp, lp if bf16 else None, ld,
+                   _arg(allow_bits, where, "allow_bits", torch.int64, dev, (R, (V + 63) // 64)), _arg(row_score, where, "row_score", f32, dev, rows),
+                   _arg(row_lse, where, "row_lse", f32, dev, rows), _arg(temperature, where, "temperature", f32, dev, requests),
+                   _arg(top_k, where, "top_k", i32, dev, requests), _arg(top_p, where, "top_p", f32, dev, requests),
+                   _arg(min_p, where, "min_p", f32, dev, requests), _arg(u, where, "u", f32, dev, (R, draws)), B, M, V, draws,
+                   _arg(out_score, where, "out_score", f32, dev), _arg(out_logq, where, "out_logq", f32, dev),
+                   _arg(out_parent, where, "out_parent", i32, dev), _arg(out_token, where, "out_token", i32, dev),
+                   _arg(d_status, where, "d_status", i32, dev), _stream()), where)
 
 
 def grace_embed(token, embed, pos, x, d_status=None):

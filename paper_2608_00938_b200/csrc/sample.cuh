@@ -264,6 +264,7 @@ struct Sampler {
   __device__ __forceinline__ int bucket_of(float x) const { return min(kSampleBuckets - 1, (int)((m - x) * c * kSampleSteps)); }
   template <class F>
   __device__ __forceinline__ void for_each(F f) const {
+#pragma unroll 2
     for (int i = tm.tid; i < row.n; i += NT) f(row.at(i), i);
   }
   __device__ __forceinline__ void note(float t, int r, int same) const {
