@@ -23,6 +23,10 @@ Pin status (what each function is checked against, besides itself):
                                     hand.
   gtm.gtm_mask                      pinned: brute force over all (row, token).
   topk.beam_topk                    pinned: python sorted() with the same key.
+  blocks.* (norm, e4m3, epilogue)   pinned: hand-worked rows, torch's e4m3
+                                    conversion on the CPU.
+  sampling.*                        pinned: hand-worked rows, the distribution
+                                    drawn by an even grid of numbers.
   decoder.beam_search               pinned: exhaustive enumeration on tiny
                                     catalogs; score monotonicity invariants.
   decoder.decoder_forward           PARITY UNPINNED against the paper: the

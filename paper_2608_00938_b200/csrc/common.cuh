@@ -47,6 +47,13 @@ __device__ __forceinline__ void flag_status(int32_t* d_status, int bits) {
   if (d_status != nullptr) atomicOr(d_status, bits);
 }
 
+// The larger of two values, NaN if either is.
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 // splitmix64 finaliser used by the prefix Bloom filter.
 __host__ __device__ __forceinline__ uint64_t mix64(uint64_t key) {
   uint64_t z = key + 0x9E3779B97F4A7C15ull;

@@ -24,12 +24,6 @@ struct CrossRowParams {
   const int32_t* enc_len;        // nullable: valid encoder positions per request
 };
 
-__device__ __forceinline__ float max_nan(float a, float b) {       // NaN if one of them is
-  float m;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
-  return m;
-}
-
 // A (row, head) pair on its own: a handful of query rows (step 0 of a decode: one beam per request; the smallest
 // searches), where the tensor-core kernels would run one 128-row tile with a few live rows through all K/V blocks in
 // sequence, and head size 32.  WARPS warps split the encoder positions of a pair (PAIRS pairs per CTA); inside a warp

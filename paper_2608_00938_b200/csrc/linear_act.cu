@@ -32,14 +32,14 @@ __device__ __forceinline__ float act_rcp(float x) {
 // An epilogue's activations are bound by the MUFU pipe (an exponential or a reciprocal is 8 clocks of a scheduler's, a
 // packed fma of two elements one slot), so a pair of elements takes two exponentials and at most one reciprocal:
 //   v / (1 + 2^s), v' / (1 + 2^s'): with a = 1 + 2^s, b = 1 + 2^s', r = 1 / (a b):  v b r and v' a r.
-// s is held at 60 (2^120 and its reciprocal are fp32 numbers): below, the results are smaller than 2^-54.
+// s is held at 60 (2^120 and its reciprocal are fp32 numbers) and v at -64 with it: beyond, the results are above -2^-54.
 // (Scalar operations: a packed one of two elements saves a slot, but takes its constants from register pairs, which cost two
 // more to fill where registers are short.)
 __device__ __forceinline__ void act_over_pair(float& v0, float& v1, float s0, float s1) {
   const float a = act_ex2(fminf(s0, 60.f)) + 1.f, b = act_ex2(fminf(s1, 60.f)) + 1.f;
   const float r = act_rcp(a * b);
-  v0 *= b * r;
-  v1 *= a * r;
+  v0 = max_nan(v0, -64.f) * (b * r);
+  v1 = max_nan(v1, -64.f) * (a * r);
 }
 __device__ __forceinline__ void act_silu(float& v0, float& v1) {
   constexpr float kLog2e = 1.4426950408889634f;
@@ -59,7 +59,7 @@ __device__ __forceinline__ float act_gelu_one(float v) {
   q = fmaf(a, q, -4.6373286843299866e-1f);
   q = fmaf(a, q, -1.149355173110962f);
   q = fmaf(a, q, -1.000108003616333f);
-  return fmaf(-a, act_ex2(q), fmaxf(v, 0.f));
+  return fmaf(-a, act_ex2(q), max_nan(v, 0.f));
 }
 __device__ __forceinline__ void act_gelu_bf16(float& v0, float& v1) { v0 = act_gelu_one(v0); v1 = act_gelu_one(v1); }
 __device__ __forceinline__ void act_gelu_f32(float& v0, float& v1) {
@@ -75,7 +75,7 @@ __device__ __forceinline__ void act_all(float (&v)[N], int act) {
     for (int i = 0; i < N; i += 2) f(v[i], v[i + 1]);
   };
   switch (act) {
-    case GRACE_ACT_RELU: all([](float& x, float& y) { x = fmaxf(x, 0.f); y = fmaxf(y, 0.f); }); break;
+    case GRACE_ACT_RELU: all([](float& x, float& y) { x = max_nan(x, 0.f); y = max_nan(y, 0.f); }); break;
     case GRACE_ACT_GELU: if constexpr (F32) all(act_gelu_f32); else all(act_gelu_bf16); break;
     case GRACE_ACT_GELU_TANH: all(act_gelu_tanh); break;
     case GRACE_ACT_SILU: all(act_silu); break;

@@ -27,12 +27,6 @@ __device__ __forceinline__ uint4 ld_once_u4(const void* p) {
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
-// The larger of two magnitudes, NaN if either is: a row with a NaN has a NaN scale, so that nothing behind takes it for numbers.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
 __device__ __forceinline__ float bf16_round(float v) { return __bfloat162float(__float2bfloat16_rn(v)); }
 
 // NT threads hold a row in pieces of eight elements, PIECES each; VEC: whole 16-byte accesses (every row of every tensor
@@ -148,7 +142,7 @@ rms_norm_kernel(const RmsParams p) {
   }
   const float rstd = rsqrtf(reduce(sq, 0) / (float)p.D + p.eps);
 
-  float most = 0.f;
+  float most = 0.f;                                        // NaN with any: a row's scale then says so
 #pragma unroll
   for (int i = 0; i < PIECES; ++i) {
     if (VEC) {

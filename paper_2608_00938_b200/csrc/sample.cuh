@@ -50,12 +50,6 @@ __device__ __forceinline__ float sample_ex2(float x) {
 }
 // A weight in 64 bits, for the rows that need them (a function of its own: e^ in 64 bits is long).
 static __device__ __noinline__ double sample_weight64(float x, float m, double inv_t) { return exp(((double)x - (double)m) * inv_t); }
-// The larger of two values, NaN if either is.
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-  return r;
-}
 
 // The threads that share a row: a warp, or a CTA.
 template <int NW>
