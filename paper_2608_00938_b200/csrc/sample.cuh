@@ -48,8 +48,10 @@ __device__ __forceinline__ float sample_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// The histogram's step of a value.
+__device__ __forceinline__ int sample_bucket(float m, float x, float c) { return min(kSampleBuckets - 1, (int)((m - x) * (c * kSampleSteps))); }
 // A weight in 64 bits, for the rows that need them (a function of its own: e^ in 64 bits is long).
-static __device__ __noinline__ double sample_weight64(float x, float m, double inv_t) { return exp(((double)x - (double)m) * inv_t); }
+static __device__ __noinline__ double sample_weight64(float x, float m, float t) { return exp(((double)x - (double)m) / (double)t); }
 
 // The threads that share a row: a warp, or a CTA.
 template <int NW>
@@ -161,11 +163,11 @@ struct LeftOut {
   RowGlobal<BF16> row;
   float bound;
   template <int NW>
-  __device__ __forceinline__ double weight64(const Team<NW> tm, float m, double inv_t) const {
+  __device__ __forceinline__ double weight64(const Team<NW> tm, float m, float temperature) const {
     double t = 0.;
     for (int i = tm.tid; i < row.n; i += NW * 32) {
       const float x = row.at(i);
-      if (x > -INFINITY && x < bound) t += sample_weight64(x, m, inv_t);
+      if (x > -INFINITY && x < bound) t += sample_weight64(x, m, temperature);
     }
     return tm.sum(t);
   }
@@ -244,7 +246,7 @@ struct Sampler {
   SampleShared<NW>* shared;
   float m;                       // largest value
   float c;                       // log2(e) / T
-  double inv_t;                  // 1 / T
+  float temperature;
   float margin;                  // of sums, relative to the whole
   int group;                     // elements of a table entry
   // top-p counts elements that the list leaves out: their weight with the list's (0: the row is all there is), and where they are
@@ -254,8 +256,8 @@ struct Sampler {
   static constexpr int kList = SampleShared<NW>::kList;
 
   __device__ __forceinline__ float weight(float x) const { return sample_ex2((x - m) * c); }
-  __device__ __forceinline__ double weight64(float x) const { return sample_weight64(x, m, inv_t); }
-  __device__ __forceinline__ int bucket_of(float x) const { return min(kSampleBuckets - 1, (int)((m - x) * c * kSampleSteps)); }
+  __device__ __forceinline__ double weight64(float x) const { return sample_weight64(x, m, temperature); }
+  __device__ __forceinline__ int bucket_of(float x) const { return sample_bucket(m, x, c); }
   template <class F>
   __device__ __forceinline__ void for_each(F f) const {
 #pragma unroll 2
@@ -266,33 +268,43 @@ struct Sampler {
   }
 
   // Narrows `cut` to its first k elements (MASS false), or to the fewest whose weights reach p of the sum of its weights.
+  // step >= 0: the histogram's step that holds the k-th, and the number of elements in front of it, are known.
   template <bool MASS>
-  static __device__ __noinline__ Cut narrow(const Sampler s, const Cut cut, const int k, const float p) { return s.template narrow_<MASS>(cut, k, p); }
+  static __device__ __noinline__ Cut narrow(const Sampler s, const Cut cut, const int k, const float p, const int step, const int step_above) {
+    return s.template narrow_<MASS>(cut, k, p, step, step_above);
+  }
   template <bool MASS>
-  __device__ __forceinline__ Cut narrow_(const Cut cut, const int k, const float p) const {
+  __device__ __forceinline__ Cut narrow_(const Cut cut, const int k, const float p, const int step, const int step_above) const {
     // fixed point: the sum of any row below 2^32
     const float scale = MASS ? exp2f(31.f - ceilf(log2f((float)row.n))) : 1.f;
     auto share = [&](float x) { return MASS ? __float2uint_rn(weight(x) * scale) : 1u; };
     tm.sync();
-    clear_hist(tm, *shared);
     if (tm.tid == 0) { shared->n_list = 0; shared->found = 0; }
-    tm.sync();
-    for_each([&](float x, int place) {
-      if (cut.keeps(x, place)) atomicAdd(&shared->hist[bucket_of(x)], share(x));
-    });
-    tm.sync();
-    auto mass_goal = [&](float want) {                     // within what the histogram holds
-      uint32_t all = 0;
-      for (int i = tm.tid; i < kSampleBuckets; i += NT) all += shared->hist[i];
-      all = tm.reduce(all, [](uint32_t a, uint32_t b) { return a + b; });
-      if (want < 0.f) want = (float)all * p;
-      return min(max(1u, (uint32_t)fminf(want, 4294967040.f)), max(1u, all));
-    };
-    find_bucket(tm, *shared, MASS ? mass_goal(whole_row > 0.f ? whole_row * scale * p : -1.f) : (uint32_t)k);
-    if (shared->bucket < 0) return cut;                         // no more than k elements
-    const int b = shared->bucket;
+    int b = step, n_above = step_above;
+    if (MASS || step < 0) {
+      clear_hist(tm, *shared);
+      tm.sync();
+      for_each([&](float x, int place) {
+        if (cut.keeps(x, place)) atomicAdd(&shared->hist[bucket_of(x)], share(x));
+      });
+      tm.sync();
+      uint32_t goal = (uint32_t)k;
+      if (MASS) {
+        uint32_t all = 0;
+        for (int i = tm.tid; i < kSampleBuckets; i += NT) all += shared->hist[i];
+        all = tm.reduce(all, [](uint32_t x, uint32_t y) { return x + y; });
+        // within what the histogram holds
+        const float want = (whole_row > 0.f ? whole_row * scale : (float)all) * p;
+        goal = min(max(1u, (uint32_t)fminf(want, 4294967040.f)), max(1u, all));
+      }
+      find_bucket(tm, *shared, goal);
+      if (shared->bucket < 0) return cut;                  // no more than k elements
+      b = shared->bucket;
+      n_above = (int)shared->above;
+    } else {
+      tm.sync();
+    }
     float whole = 0.f, above = 0.f;
-    int n_above = (int)shared->above;
     for_each([&](float x, int place) {
       if (!cut.keeps(x, place)) return;
       const int at = bucket_of(x);
@@ -472,7 +484,7 @@ struct Sampler {
       if (x > top) above += w;
     });
     whole = tm.sum(whole);
-    if (whole_row > 0.f) whole += rest.weight64(tm, m, inv_t);
+    if (whole_row > 0.f) whole += rest.weight64(tm, m, temperature);
     above = tm.sum(above);
     const double goal = (double)p * whole;
     auto settle = [&](float x, double front, int same) {
@@ -635,10 +647,13 @@ struct RowLimits {
   float temperature, top_p, min_p;
   int top_k;
   float score, lse, u;           // u: this thread's first draw
+  int beam;
+  int step = -1, step_above = 0; // top-k: the histogram's step that holds the k-th, where it is known
 };
 __device__ __forceinline__ RowLimits row_limits(const SampleParams& p, int64_t r, int tid) {
-  const int b = (int)(r / p.M);
+  const uint32_t b = (uint32_t)r / (uint32_t)p.M;          // (rows are below 2^31)
   RowLimits l;
+  l.beam = (int)((uint32_t)r - b * (uint32_t)p.M);
   l.temperature = p.temperature != nullptr ? __ldg(p.temperature + b) : 1.f;
   l.top_k = p.top_k != nullptr ? __ldg(p.top_k + b) : 0;
   l.top_p = p.top_p != nullptr ? __ldg(p.top_p + b) : 1.f;
@@ -649,23 +664,18 @@ __device__ __forceinline__ RowLimits row_limits(const SampleParams& p, int64_t r
   return l;
 }
 struct Scale {                   // of the weights
-  double t64, inv_t;
-  float c;
-  __device__ __forceinline__ explicit Scale(float temperature) {
-    t64 = fmin((double)temperature, 1e30);
-    inv_t = 1. / t64;
-    c = (float)fmin(1.4426950408889634 * inv_t, 1e38);
-  }
+  float t, c;                    // T, log2(e) / T
+  __device__ __forceinline__ explicit Scale(float temperature) : t(fminf(temperature, 1e30f)), c(fminf(1.44269504f / t, 1e38f)) {}
 };
 // w >= min_p as a bound on x, rounded up to the next fp32.
-__device__ __forceinline__ float min_p_bound(float m, float min_p, double t64) {
-  return min_p < 1.f ? fminf(m, __double2float_ru((double)m + t64 * log((double)min_p))) : m;
+__device__ __forceinline__ float min_p_bound(float m, float min_p, float t) {
+  return min_p < 1.f ? fminf(m, __double2float_ru((double)m + (double)t * log((double)min_p))) : m;
 }
 // x: the token's logit
 __device__ __forceinline__ void store_draw(const SampleParams& p, const RowLimits& l, int64_t r, int d, int token, float x, float logq) {
   const int64_t at = r * p.draws + d;
   p.out_token[at] = token;
-  if (p.out_parent != nullptr) p.out_parent[at] = (int)(r % p.M);
+  if (p.out_parent != nullptr) p.out_parent[at] = l.beam;
   p.out_score[at] = logq == -INFINITY ? -INFINITY : l.score + (x - l.lse);
   if (p.out_logq != nullptr) p.out_logq[at] = logq;
 }
@@ -680,12 +690,12 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
                                                const RowLimits& l, const Scale& sc, float whole_row, const LeftOut<BF16>& rest, bool infinite) {
   constexpr int NT = NW * 32;
   using S = Sampler<NW, Row, LeftOut<BF16>>;
-  const S s{row, tm, &sh, m, sc.c, sc.inv_t, p.V > 2048 ? 0x1p-17f : 0x1p-18f, (row.n + 4 * NT - 1) / (4 * NT), whole_row, rest};
+  const S s{row, tm, &sh, m, sc.c, sc.t, p.V > 2048 ? 0x1p-17f : 0x1p-18f, (row.n + 4 * NT - 1) / (4 * NT), whole_row, rest};
   Cut cut = {-INFINITY, -1};
-  if (l.top_k > 0 && l.top_k < row.n) cut = S::template narrow<false>(s, cut, l.top_k, 0.f);
-  if (l.top_p < 1.f) cut = S::template narrow<true>(s, cut, 0, fmaxf(l.top_p, 0.f));
+  if (l.top_k > 0 && l.top_k < row.n) cut = S::template narrow<false>(s, cut, l.top_k, 0.f, l.step, l.step_above);
+  if (l.top_p < 1.f) cut = S::template narrow<true>(s, cut, 0, fmaxf(l.top_p, 0.f), -1, 0);
   if (l.min_p > 0.f) {
-    const float least = min_p_bound(m, l.min_p, sc.t64);
+    const float least = min_p_bound(m, l.min_p, sc.t);
     if (least > cut.t) cut = Cut{least, 0x7fffffff};
   }
   float* table32 = reinterpret_cast<float*>(sh.table);
@@ -694,7 +704,7 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
   auto store = [&](int d, int place) {
     place = max(place, 0);
     const float x = row.at(place);
-    store_draw(p, l, r, d, row.token(place), infinite ? INFINITY : x, (float)(((double)x - (double)m) * sc.inv_t) - log_whole);
+    store_draw(p, l, r, d, row.token(place), infinite ? INFINITY : x, (x - m) / sc.t - log_whole);
   };
   bool have64 = false;
   // few draws: a warp together for one after the other; many: each thread its own
@@ -723,7 +733,7 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
 // place and is narrowed there; otherwise every pass reads it.
 template <int NW, bool BF16, bool SHARED>
 __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF16> row, const Team<NW>& tm, SampleShared<NW>& sh, float* vals,
-                                             uint16_t* tokens, int64_t r, int n, const RowLimits& l) {
+                                             uint16_t* tokens, int64_t r, int n, RowLimits l) {
   constexpr int NT = NW * 32;
   const int lane = tm.tid & 31, warp = tm.tid >> 5;
   // a warp's quads are neighbours, lane by lane: `iters` of 32
@@ -790,26 +800,29 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   const Scale sc(l.temperature);
   // a bound below which nothing is kept (and nothing counts: top-p's sum is that of the top_k, whatever min-p leaves of them)
   const bool by_count = l.top_k > 0 && l.top_k < n, by_mass = !by_count && l.top_p < 1.f;
-  float bound = l.min_p > 0.f && !(by_count && l.top_p < 1.f) ? min_p_bound(m, l.min_p, sc.t64) : -INFINITY;
+  float bound = l.min_p > 0.f && !(by_count && l.top_p < 1.f) ? min_p_bound(m, l.min_p, sc.t) : -INFINITY;
   float whole_row = 0.f;
   if (by_count) {
     clear_hist(tm, sh);
     tm.sync();
-    const float cs = sc.c * kSampleSteps;
     auto count = [&](float x) {
-      if (x > -INFINITY) atomicAdd(&sh.hist[min(kSampleBuckets - 1, (int)((m - x) * cs))], 1u);
+      if (x > -INFINITY) atomicAdd(&sh.hist[sample_bucket(m, x, sc.c)], 1u);
     };
+#pragma unroll (SHARED ? 1 : 4)
     for (int i = 0; i < iters; ++i) {
       const float4 t = quad(first + 32 * i);
       count(t.x); count(t.y); count(t.z); count(t.w);
     }
     tm.sync();
     find_bucket(tm, sh, (uint32_t)l.top_k);
-    const int b = sh.bucket;
+    l.step = sh.bucket;
+    l.step_above = (int)sh.above;
     // the step's far edge, further by what rounding can make of it
-    if (b >= 0 && b < kSampleBuckets - 1) bound = fmaxf(bound, m - ((float)(b + 1) * 1.0001f) / cs - fabsf(m) * 0x1p-20f);
+    if (l.step >= 0 && l.step < kSampleBuckets - 1)
+      bound = fmaxf(bound, m - ((float)(l.step + 1) * 1.0001f) / (sc.c * kSampleSteps) - fabsf(m) * 0x1p-20f);
   } else if (by_mass) {
     float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll 4
     for (int i = 0; i < iters; ++i) {
       const float4 t = quad(first + 32 * i);
       s0 += sample_ex2((t.x - m) * sc.c); s1 += sample_ex2((t.y - m) * sc.c);
