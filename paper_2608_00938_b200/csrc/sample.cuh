@@ -200,10 +200,10 @@ struct SampleShared {
   int len, copies, pad[1];
 };
 
-// First step at which the histogram's running sum reaches `target` (sh.bucket) and the sum in front of it (sh.above);
+// First step at which the histogram's running sum reaches goal(its whole sum) (sh.bucket) and the sum in front of it (sh.above);
 // -1 if none does.
-template <int NW>
-__device__ __forceinline__ void find_bucket(const Team<NW>& tm, SampleShared<NW>& sh, uint32_t target) {
+template <int NW, class Goal>
+__device__ __forceinline__ void find_bucket(const Team<NW>& tm, SampleShared<NW>& sh, Goal goal) {
   if (tm.tid < 32) {
     const int lane = tm.tid;
     const uint4 lo = reinterpret_cast<const uint4*>(sh.hist)[2 * lane], hi = reinterpret_cast<const uint4*>(sh.hist)[2 * lane + 1];
@@ -215,6 +215,7 @@ __device__ __forceinline__ void find_bucket(const Team<NW>& tm, SampleShared<NW>
       const uint32_t t = __shfl_up_sync(kFullMask, incl, o);
       if (lane >= o) incl += t;
     }
+    const uint32_t target = goal(__shfl_sync(kFullMask, incl, 31));
     const uint32_t reached = __ballot_sync(kFullMask, incl >= target);
     if (reached == 0u) {
       if (lane == 0) sh.bucket = -1;
@@ -270,13 +271,9 @@ struct Sampler {
   // Narrows `cut` to its first k elements (MASS false), or to the fewest whose weights reach p of the sum of its weights.
   // step >= 0: the histogram's step that holds the k-th, and the number of elements in front of it, are known.
   template <bool MASS>
-  static __device__ __noinline__ Cut narrow(const Sampler s, const Cut cut, const int k, const float p, const int step, const int step_above) {
-    return s.template narrow_<MASS>(cut, k, p, step, step_above);
-  }
-  template <bool MASS>
-  __device__ __forceinline__ Cut narrow_(const Cut cut, const int k, const float p, const int step, const int step_above) const {
+  __device__ __forceinline__ Cut narrow(const Cut cut, const int k, const float p, const int step, const int step_above) const {
     // fixed point: the sum of any row below 2^32
-    const float scale = MASS ? exp2f(31.f - ceilf(log2f((float)row.n))) : 1.f;
+    const float scale = MASS ? __uint_as_float((uint32_t)(126 + __clz(row.n - 1)) << 23) : 1.f;   // 2^(31 - ceil(log2 n))
     auto share = [&](float x) { return MASS ? __float2uint_rn(weight(x) * scale) : 1u; };
     tm.sync();
     if (tm.tid == 0) { shared->n_list = 0; shared->found = 0; }
@@ -288,16 +285,12 @@ struct Sampler {
         if (cut.keeps(x, place)) atomicAdd(&shared->hist[bucket_of(x)], share(x));
       });
       tm.sync();
-      uint32_t goal = (uint32_t)k;
-      if (MASS) {
-        uint32_t all = 0;
-        for (int i = tm.tid; i < kSampleBuckets; i += NT) all += shared->hist[i];
-        all = tm.reduce(all, [](uint32_t x, uint32_t y) { return x + y; });
+      find_bucket(tm, *shared, [&](uint32_t all) {
+        if (!MASS) return (uint32_t)k;
         // within what the histogram holds
         const float want = (whole_row > 0.f ? whole_row * scale : (float)all) * p;
-        goal = min(max(1u, (uint32_t)fminf(want, 4294967040.f)), max(1u, all));
-      }
-      find_bucket(tm, *shared, goal);
+        return min(max(1u, (uint32_t)fminf(want, 4294967040.f)), max(1u, all));
+      });
       if (shared->bucket < 0) return cut;                  // no more than k elements
       b = shared->bucket;
       n_above = (int)shared->above;
@@ -428,14 +421,9 @@ struct Sampler {
         if (key >= key_lo && key <= key_hi && cut.keeps(x, place)) atomicAdd(&shared->hist[(key_hi - key) >> shift], MASS ? __float2uint_rn(weight(x) * scale) : 1u);
       });
       tm.sync();
-      uint32_t want = (uint32_t)(k - n_above);
-      if (MASS) {
-        uint32_t all = 0;
-        for (int i = tm.tid; i < kSampleBuckets; i += NT) all += shared->hist[i];
-        all = tm.reduce(all, [](uint32_t a, uint32_t d) { return a + d; });
-        want = min((uint32_t)fminf(fmaxf((p * whole - above) * scale, 1.f), 4294967040.f), max(1u, all));
-      }
-      find_bucket(tm, *shared, want);
+      find_bucket(tm, *shared, [&](uint32_t all) {
+        return MASS ? min((uint32_t)fminf(fmaxf((p * whole - above) * scale, 1.f), 4294967040.f), max(1u, all)) : (uint32_t)(k - n_above);
+      });
       const int at = max(0, shared->bucket);
       key_hi -= (uint32_t)at << shift;
       key_lo = max(key_lo, key_hi - ((1u << shift) - 1u));
@@ -543,7 +531,15 @@ struct Sampler {
   __device__ __forceinline__ F tabulate(const Cut cut, F* table) const {
     tm.sync();
     F s = F(0);
+#pragma unroll 1
     for (int e = 0; e < 4; ++e) {
+      if (group == 1) {                                    // a short list
+        const int i = 4 * tm.tid + e;
+        const F t = i < row.n ? kept_weight<F>(cut, i) : F(0);
+        table[i] = t;
+        s += t;
+        continue;
+      }
       F t = F(0);
       const int i0 = (4 * tm.tid + e) * group;
       // each thread from another of its elements on, round once: side by side they would all be on one bank
@@ -692,8 +688,8 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
   using S = Sampler<NW, Row, LeftOut<BF16>>;
   const S s{row, tm, &sh, m, sc.c, sc.t, p.V > 2048 ? 0x1p-17f : 0x1p-18f, (row.n + 4 * NT - 1) / (4 * NT), whole_row, rest};
   Cut cut = {-INFINITY, -1};
-  if (l.top_k > 0 && l.top_k < row.n) cut = S::template narrow<false>(s, cut, l.top_k, 0.f, l.step, l.step_above);
-  if (l.top_p < 1.f) cut = S::template narrow<true>(s, cut, 0, fmaxf(l.top_p, 0.f), -1, 0);
+  if (l.top_k > 0 && l.top_k < row.n) cut = s.template narrow<false>(cut, l.top_k, 0.f, l.step, l.step_above);
+  if (l.top_p < 1.f) cut = s.template narrow<true>(cut, 0, fmaxf(l.top_p, 0.f), -1, 0);
   if (l.min_p > 0.f) {
     const float least = min_p_bound(m, l.min_p, sc.t);
     if (least > cut.t) cut = Cut{least, 0x7fffffff};
@@ -740,7 +736,8 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   const int quads = (p.V + 3) >> 2, iters = (quads + NT - 1) / NT, first = warp * 32 * iters + lane;
   float4* const shared = reinterpret_cast<float4*>(vals);
   auto none = []() { return make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY); };
-  auto quad = [&](int q) { return q < quads ? (SHARED ? shared[q] : row.quad(q)) : none(); };
+  // (SHARED: filled up to whole passes with -inf)
+  auto quad = [&](int q) { return SHARED ? shared[q] : (q < quads ? row.quad(q) : none()); };
   float m = -INFINITY;
   auto see = [&](const float4& t) { m = max_nan(m, max_nan(max_nan(t.x, t.y), max_nan(t.z, t.w))); };
   int i0 = 0;
@@ -765,7 +762,7 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       see(t[i]);
-      if (SHARED && i0 + i < iters && first + 32 * (i0 + i) < quads) shared[first + 32 * (i0 + i)] = t[i];
+      if (SHARED && i0 + i < iters) shared[first + 32 * (i0 + i)] = t[i];
     }
   }
   m = tm.reduce(m, [](float a, float b) { return max_nan(a, b); });
@@ -781,7 +778,8 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
     if (SHARED) {
       for (int i = 0; i < iters; ++i) {
         const int q = first + 32 * i;
-        if (q < quads) { const float4 t = shared[q]; shared[q] = make_float4(row.shown(t.x), row.shown(t.y), row.shown(t.z), row.shown(t.w)); }
+        const float4 t = shared[q];
+        shared[q] = make_float4(row.shown(t.x), row.shown(t.y), row.shown(t.z), row.shown(t.w));
       }
     }
   }
@@ -814,7 +812,7 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
       count(t.x); count(t.y); count(t.z); count(t.w);
     }
     tm.sync();
-    find_bucket(tm, sh, (uint32_t)l.top_k);
+    find_bucket(tm, sh, [&](uint32_t) { return (uint32_t)l.top_k; });
     l.step = sh.bucket;
     l.step_above = (int)sh.above;
     // the step's far edge, further by what rounding can make of it
@@ -834,6 +832,27 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   }
   if (by_count || by_mass || l.min_p > 0.f) {
     bound = fmaxf(fminf(bound, m), -3.402823466e38f);      // (-inf is in no list)
+    if constexpr (SHARED) {
+      // 32 neighbours at a time, in place: the list is never ahead of what has been read.  One that outgrows its tokens' room
+      // is given up, and the row read again.
+      __syncwarp();
+      int kept = 0;
+#pragma unroll 4
+      for (int i = 0; i < 4 * iters; ++i) {
+        const float x = vals[32 * i + lane];
+        const uint32_t in = __ballot_sync(kFullMask, x >= bound);
+        const int at = kept + __popc(in & ((1u << lane) - 1u));
+        if (x >= bound && at < p.tokens_cap) { vals[at] = x; tokens[at] = (uint16_t)(32 * i + lane); }
+        kept += __popc(in);
+      }
+      __syncwarp();
+      if (kept <= p.tokens_cap) {
+        const RowShared list{vals, tokens, kept};
+        limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, sc, whole_row, LeftOut<BF16>{row, bound}, row.inf);
+        return;
+      }
+      for (int i = 0; i < iters; ++i) shared[first + 32 * i] = first + 32 * i < quads ? row.quad(first + 32 * i) : none();
+    } else {
     // Four quads at a time: counts in the bytes of a word, summed over the lanes at once.
     static_assert(kSampleMostV <= 4 * 32 * 32 * 16, "");   // at most 16 quads a thread
     uint32_t counts[4] = {0, 0, 0, 0};
@@ -861,7 +880,6 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
       kept = starts[NW - 1];
     }
     if (kept <= p.tokens_cap) {
-      // In place (SHARED, one warp) the list never reaches the quads that are still to be read.
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         if (4 * g >= iters) break;
@@ -892,6 +910,7 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
       const RowShared list{vals, tokens, kept};
       limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, sc, whole_row, LeftOut<BF16>{row, bound}, row.inf);
       return;
+    }
     }
   }
   // no limit, or one that leaves more than a list takes: the whole row
@@ -1003,7 +1022,7 @@ static grace_status_t launch_sample(SampleParams p, cudaStream_t s) {
   // for half the tokens; a row with more allowed ones is read by every pass, as are longer rows.
   constexpr bool kShared = NW == 1 && !LISTS;
   constexpr int kTeams = NW == 1 ? 2 : 1;
-  const int row = (p.V + 15) & ~15, half = p.V <= 512 ? row : (p.V / 2 + 15) & ~15;
+  const int row = kShared ? (p.V + 127) & ~127 : (p.V + 15) & ~15, half = p.V <= 512 ? row : (p.V / 2 + 15) & ~15;
   p.cap = NW == 32 ? 16384 : (LISTS ? half : row);
   p.tokens_cap = NW == 32 ? 16384 : half;
   p.team_bytes = ((int)sizeof(SampleShared<NW>) + p.cap * 4 + p.tokens_cap * 2 + 15) & ~15;
