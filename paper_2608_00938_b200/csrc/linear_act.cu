@@ -5,6 +5,7 @@
 // tiles, swizzle, descriptors and the dispatch rule of linear_form.cuh; an e4m3 product has half the k-blocks.
 // act_kernel: one 128 x BN tile per CTA or per cluster that shares its K range.  act_pair_kernel: persistent CTA pairs on
 // 256 x 256 tiles, two accumulators in TMEM, the epilogue of one under the products of the other.
+#include <algorithm>
 #include "common.cuh"
 #include "linear_form.cuh"
 #include "tc.cuh"
@@ -17,6 +18,7 @@ struct ActParams {
   void* y;
   int64_t ldr, ldy;
   int M, N, KB, act;                                       // KB: k-blocks (the last one filled up with zeros)
+  int bn;                                                  // act_pair_kernel: columns of a tile
 };
 
 __device__ __forceinline__ float act_ex2(float x) {
@@ -320,7 +322,7 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 }
 
 // ---------------------------------------------------------------------------------------------
-// Persistent CTA pairs: 256 x 256 tiles (n fastest), each CTA with 128 rows of x and 128 of the tile's rows of w in a ring of
+// Persistent CTA pairs: tiles of 256 x bn (n fastest), each CTA with 128 rows of x and bn / 2 of the tile's rows of w in a ring of
 // five stages, one tcgen05.mma stream per pair into one of two accumulators (all of TMEM).
 // Epilogue: sixteen warps per CTA, each with 32 rows x 64 columns of its own.  A thread has a row: it takes a step's columns
 // (32 of a bf16 result, 16 of an fp32 one) out of the accumulator, finishes them and leaves them in the warp's 2 KB of shared
@@ -382,7 +384,7 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = tc::cluster_cta_rank();            // 0: issues the MMAs; 1: peer
   const int pair = blockIdx.x >> 1, n_pairs = gridDim.x >> 1;
-  const int n_tiles = (p.N + 255) / 256, total = n_tiles * ((p.M + 255) / 256);
+  const int n_tiles = (p.N + p.bn - 1) / p.bn, total = n_tiles * ((p.M + 255) / 256);
   constexpr int kBK = F8 ? 128 : 64;
 
   if (threadIdx.x == 0) {
@@ -406,11 +408,11 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     if (lane == 0) {                                        // ---- TMA producer (both CTAs) ----
       int it = 0;
       for (int tile = pair; tile < total; tile += n_pairs) {
-        const int m0 = (tile / n_tiles) * 256 + (int)rank * 128, n0 = (tile % n_tiles) * 256 + (int)rank * 128;
+        const int m0 = (tile / n_tiles) * 256 + (int)rank * 128, n0 = (tile % n_tiles) * p.bn + (int)rank * (p.bn / 2);
         for (int kb = 0; kb < p.KB; ++kb, ++it) {
           const int s = it % kAPStages;
           if (!tc::mbar_wait_cluster(empty + s, ((it / kAPStages) & 1) ^ 1, abort_flag)) { tile = total; break; }
-          if (rank == 0) tc::mbar_expect_tx(full + s, 2 * kAPStageBytes);    // this CTA's bytes and the peer's
+          if (rank == 0) tc::mbar_expect_tx(full + s, 2 * (128 * 128 + p.bn / 2 * 128));   // this CTA's bytes and the peer's
           uint8_t* a = tiles + s * kAPStageBytes;
           const uint32_t bar = tc::cluster_addr_of(full + s, 0);
           tc::tma_load_2d_pair(a, &map_x, bar, kb * kBK, m0);
@@ -420,7 +422,7 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     }
   } else if (warp == 1) {
     if (lane == 0 && rank == 0) {                           // ---- even CTA: MMA issuer for the pair ----
-      constexpr uint32_t idesc = act_idesc<F8>(256, 256);
+      const uint32_t idesc = act_idesc<F8>(256, p.bn);
       int it = 0, local = 0;
       for (int tile = pair; tile < total; tile += n_pairs, ++local) {
         const int ab = local & 1;
@@ -493,12 +495,12 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     // the next tile's coordinates without a division
     const int step_m = n_pairs / n_tiles, step_n = n_pairs % n_tiles;
     int tile_m = pair / n_tiles, tile_n = pair % n_tiles;
-    int m0 = tile_m * 256 + (int)rank * 128 + q * 32, n0 = tile_n * 256 + col;
+    int m0 = tile_m * 256 + (int)rank * 128 + q * 32, n0 = tile_n * p.bn + col;
     fetch(m0, n0);
     int local = 0;
     for (int tile = pair; tile < total; tile += n_pairs, ++local) {
       m0 = tile_m * 256 + (int)rank * 128 + q * 32;
-      n0 = tile_n * 256 + col;
+      n0 = tile_n * p.bn + col;
       tile_m += step_m;
       tile_n += step_n;
       if (tile_n >= n_tiles) { tile_n -= n_tiles; ++tile_m; }
@@ -511,7 +513,7 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         if (F8) scale[32 * i + lane] = ws_next[i];
         scale[kAPWarpCols + 32 * i + lane] = bias_next[i];
       }
-      fetch(tile_m * 256 + (int)rank * 128 + q * 32, tile_n * 256 + col);
+      fetch(tile_m * 256 + (int)rank * 128 + q * 32, tile_n * p.bn + col);
       bool ok = tc::mbar_wait_cluster(acc_full + ab, (local >> 1) & 1, abort_flag);
       ok = __all_sync(kFullMask, ok);
       if (!ok) break;
@@ -530,7 +532,7 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             else tc::mbar_arrive_remote(acc_empty + ab, 0);
           }
         }
-        if (m0 >= p.M || n0 + c0 >= p.N) continue;          // the same for the whole warp
+        if (m0 >= p.M || n0 + c0 >= p.N || col + c0 >= p.bn) continue;             // the same for the whole warp
         float v[kCols];
         act_affine<F8>(v, r, xs, scale + c0);
         act_all<F32>(v, p.act);
@@ -647,7 +649,7 @@ static grace_status_t launch_act_pair(const CUtensorMap& mx, const CUtensorMap& 
     max_clusters_of[su.dev] = clusters < n_sm / 2 ? clusters : n_sm / 2;
     su.done();
   }
-  const int64_t total = (int64_t)((p.N + 255) / 256) * ((p.M + 255) / 256);
+  const int64_t total = (int64_t)((p.N + p.bn - 1) / p.bn) * ((p.M + 255) / 256);
   const int most = max_clusters_of[su.dev];
   cfg.gridDim = dim3(2 * (unsigned)(total < most ? total : most));
   GRACE_CUDA_TRY(cudaLaunchKernelEx(&cfg, act_pair_kernel<F8, F32, WIDE>, mx, mw, my, p));
@@ -670,6 +672,22 @@ static grace_status_t run_act(const LinearForm& f, const CUtensorMap& mx, const 
     case 128 * 16 + 3: return launch_act<F8, F32, 128, 3, 1>(mx, mw, p, s);
   }
   return GRACE_UNSUPPORTED_SHAPE;
+}
+
+// Columns of the CTA pairs' tiles: a narrower tile where fewer of the last wave's pairs then stay without one.  A k-block of a
+// tile takes 256 + bn clocks (16 KB of x and 64 bn bytes of w through a port of 64 bytes a clock), its epilogue about 6400 whatever bn
+// (a warp has 64 columns or none); whichever is more, times the waves.  (Taken in turn, 256 columns and these:
+// 6000 x 1100 x 4096 bf16 52.3 -> 49.2 us, 9000 x 777 x 4096 52.9 -> 50.3, 10000 x 512 x 8192 89.0 -> 87.6; a loss of 1.5 % at
+// 7003 x 2036 x 8184, 233.7 -> 237.3, where the clock gives way to the power limit.)
+static int act_pair_columns(int M, int N, int KB) {
+  int best = 256;
+  int64_t least = INT64_MAX;
+  for (int bn = 256; bn >= 128; bn -= 32) {
+    const int64_t tiles = (int64_t)((M + 255) / 256) * ((N + bn - 1) / bn), waves = (tiles + kSmsInTwos / 2 - 1) / (kSmsInTwos / 2);
+    const int64_t one = std::max((int64_t)KB * (256 + bn), (int64_t)6400), t = waves * one;
+    if (t < least) { least = t; best = bn; }
+  }
+  return best;
 }
 
 template <bool F8>
@@ -696,7 +714,8 @@ static grace_status_t linear_act_impl(const void* x, int64_t ldx, const float* x
   const CUtensorMapDataType type = F8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   CUtensorMap mx, mw;
   const uint64_t dx[2] = {(uint64_t)K, (uint64_t)M}, sx[1] = {(uint64_t)ldx}, dw[2] = {(uint64_t)K, (uint64_t)N}, sw[1] = {(uint64_t)ldw};
-  const uint32_t bx[2] = {(uint32_t)kBK, 128u}, bw[2] = {(uint32_t)kBK, form.bn == 0 ? 128u : (uint32_t)form.bn};
+  p.bn = act_pair_columns(M, N, p.KB);
+  const uint32_t bx[2] = {(uint32_t)kBK, 128u}, bw[2] = {(uint32_t)kBK, form.bn == 0 ? (uint32_t)p.bn / 2 : (uint32_t)form.bn};
   if (!tc::make_tmap_typed(&mx, x, 2, dx, sx, bx, type, kEsize) || !tc::make_tmap_typed(&mw, w, 2, dw, sw, bw, type, kEsize)) return GRACE_CUDA_ERROR;
   if (form.bn != 0) return f32 ? run_act<F8, true>(form, mx, mw, p, s) : run_act<F8, false>(form, mx, mw, p, s);
   const bool wide = ((reinterpret_cast<uintptr_t>(y) | (uintptr_t)(ldy * size)) & 15) == 0 &&

@@ -110,6 +110,7 @@ __device__ __forceinline__ float logit_at(const char* row, int token) {
 
 // A row's elements in the order of their tokens: in shared memory (`tokens` NULL: element i is token i), ...
 struct RowShared {
+  static constexpr bool kQuads = false;
   const float* vals;
   const uint16_t* tokens;
   int n;
@@ -119,6 +120,7 @@ struct RowShared {
 // ... or where they are, read again by every pass (out of L2): a row of which more stays than a list takes.
 template <bool BF16>
 struct RowGlobal {
+  static constexpr bool kQuads = true;
   const char* row;
   const uint64_t* allow;
   int n, vec;
@@ -165,9 +167,13 @@ struct LeftOut {
   template <int NW>
   __device__ __forceinline__ double weight64(const Team<NW> tm, float m, float temperature) const {
     double t = 0.;
-    for (int i = tm.tid; i < row.n; i += NW * 32) {
-      const float x = row.at(i);
-      if (x > -INFINITY && x < bound) t += sample_weight64(x, m, temperature);
+#pragma unroll 2
+    for (int q = tm.tid; q < (row.n + 3) >> 2; q += NW * 32) {
+      const float4 v = row.quad(q);
+      const float most = fmaxf(fmaxf(v.x < bound ? v.x : -INFINITY, v.y < bound ? v.y : -INFINITY), fmaxf(v.z < bound ? v.z : -INFINITY, v.w < bound ? v.w : -INFINITY));
+      if ((most - m) / temperature < -80.f) continue;      // (lighter than 2^-115 each)
+      auto left = [&](float x) { return x < bound ? exp(((double)x - (double)m) / (double)temperature) : 0.; };
+      t += (left(v.x) + left(v.y)) + (left(v.z) + left(v.w));
     }
     return tm.sum(t);
   }
@@ -542,6 +548,16 @@ struct Sampler {
       }
       F t = F(0);
       const int i0 = (4 * tm.tid + e) * group;
+      if constexpr (Row::kQuads) {                         // in memory: whole quads
+        for (int q = i0 >> 2; q < min(i0 + group, (row.n + 3) & ~3) >> 2; ++q) {
+          const float4 v = row.quad(q);
+          auto kept = [&](float x, int j) { return cut.keeps(x, 4 * q + j) ? (sizeof(F) == 8 ? (F)weight64(x) : (F)weight(x)) : F(0); };
+          t += (kept(v.x, 0) + kept(v.y, 1)) + (kept(v.z, 2) + kept(v.w, 3));
+        }
+        table[4 * tm.tid + e] = t;
+        s += t;
+        continue;
+      }
       // each thread from another of its elements on, round once: side by side they would all be on one bank
       int k = tm.tid % group;
       for (int i = 0; i < group; ++i) {
@@ -645,6 +661,7 @@ struct RowLimits {
   float score, lse, u;           // u: this thread's first draw
   int beam;
   int step = -1, step_above = 0; // top-k: the histogram's step that holds the k-th, where it is known
+  float least = -INFINITY;       // min-p's bound on x
 };
 __device__ __forceinline__ RowLimits row_limits(const SampleParams& p, int64_t r, int tid) {
   const uint32_t b = (uint32_t)r / (uint32_t)p.M;          // (rows are below 2^31)
@@ -686,14 +703,16 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
                                                const RowLimits& l, const Scale& sc, float whole_row, const LeftOut<BF16>& rest, bool infinite) {
   constexpr int NT = NW * 32;
   using S = Sampler<NW, Row, LeftOut<BF16>>;
-  const S s{row, tm, &sh, m, sc.c, sc.t, p.V > 2048 ? 0x1p-17f : 0x1p-18f, (row.n + 4 * NT - 1) / (4 * NT), whole_row, rest};
+  // Sums' worst error, relative to the whole.  A weight's: its exponent's, 3.5 x 2^-24 of z = (max - x) / T (the difference, c, the
+  // product), whose mean over the weights is at most ln V (a distribution's entropy is); 2^-22 of ex2.  A sum's: 2^-24 for each of
+  // the 30 additions that an addend passes at most.  V 2048: 3.3e-6, V 65536: 4.4e-6.
+  const float margin = p.V > 2048 ? 4.5e-6f : 3.4e-6f;
+  const int group = (row.n + 4 * NT - 1) / (4 * NT);
+  const S s{row, tm, &sh, m, sc.c, sc.t, margin, Row::kQuads ? (group + 3) & ~3 : group, whole_row, rest};
   Cut cut = {-INFINITY, -1};
   if (l.top_k > 0 && l.top_k < row.n) cut = s.template narrow<false>(cut, l.top_k, 0.f, l.step, l.step_above);
   if (l.top_p < 1.f) cut = s.template narrow<true>(cut, 0, fmaxf(l.top_p, 0.f), -1, 0);
-  if (l.min_p > 0.f) {
-    const float least = min_p_bound(m, l.min_p, sc.t);
-    if (least > cut.t) cut = Cut{least, 0x7fffffff};
-  }
+  if (l.least > cut.t) cut = Cut{l.least, 0x7fffffff};
   float* table32 = reinterpret_cast<float*>(sh.table);
   const float whole = s.template tabulate<float>(cut, table32);
   const float log_whole = logf(whole);
@@ -798,7 +817,8 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   const Scale sc(l.temperature);
   // a bound below which nothing is kept (and nothing counts: top-p's sum is that of the top_k, whatever min-p leaves of them)
   const bool by_count = l.top_k > 0 && l.top_k < n, by_mass = !by_count && l.top_p < 1.f;
-  float bound = l.min_p > 0.f && !(by_count && l.top_p < 1.f) ? min_p_bound(m, l.min_p, sc.t) : -INFINITY;
+  if (l.min_p > 0.f) l.least = min_p_bound(m, l.min_p, sc.t);
+  float bound = by_count && l.top_p < 1.f ? -INFINITY : l.least;
   float whole_row = 0.f;
   if (by_count) {
     clear_hist(tm, sh);
@@ -833,17 +853,28 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   if (by_count || by_mass || l.min_p > 0.f) {
     bound = fmaxf(fminf(bound, m), -3.402823466e38f);      // (-inf is in no list)
     if constexpr (SHARED) {
-      // 32 neighbours at a time, in place: the list is never ahead of what has been read.  One that outgrows its tokens' room
+      // 128 neighbours at a time, in place: the list is never ahead of what has been read.  One that outgrows its tokens' room
       // is given up, and the row read again.
       __syncwarp();
       int kept = 0;
-#pragma unroll 4
-      for (int i = 0; i < 4 * iters; ++i) {
-        const float x = vals[32 * i + lane];
-        const uint32_t in = __ballot_sync(kFullMask, x >= bound);
-        const int at = kept + __popc(in & ((1u << lane) - 1u));
-        if (x >= bound && at < p.tokens_cap) { vals[at] = x; tokens[at] = (uint16_t)(32 * i + lane); }
-        kept += __popc(in);
+      const uint32_t to_vals = (uint32_t)__cvta_generic_to_shared(vals), to_tokens = (uint32_t)__cvta_generic_to_shared(tokens);
+      const uint32_t below = (1u << lane) - 1u;
+      auto take = [&](float x, uint32_t& at, int token) {
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ge.f32 p, %3, %4;\n\t@p st.shared.f32 [%1], %3;\n\t@p st.shared.u16 [%2], %5;\n\t@p add.u32 %0, %0, 1;\n\t}"
+                     : "+r"(at) : "r"(to_vals + 4 * at), "r"(to_tokens + 2 * at), "f"(x), "f"(bound), "h"((uint16_t)token) : "memory");
+      };
+#pragma unroll 2
+      for (int i = 0; i < iters; ++i) {
+        const float4 t = shared[32 * i + lane];
+        const uint32_t b0 = __ballot_sync(kFullMask, t.x >= bound), b1 = __ballot_sync(kFullMask, t.y >= bound), b2 = __ballot_sync(kFullMask, t.z >= bound),
+                       b3 = __ballot_sync(kFullMask, t.w >= bound);
+        const int all = (__popc(b0) + __popc(b1)) + (__popc(b2) + __popc(b3));
+        if (all == 0) continue;
+        uint32_t at = (uint32_t)(kept + (__popc(b0 & below) + __popc(b1 & below)) + (__popc(b2 & below) + __popc(b3 & below)));
+        kept += all;
+        if (kept > p.tokens_cap) break;
+        const int token = 4 * (32 * i + lane);
+        take(t.x, at, token); take(t.y, at, token + 1); take(t.z, at, token + 2); take(t.w, at, token + 3);
       }
       __syncwarp();
       if (kept <= p.tokens_cap) {
@@ -943,7 +974,7 @@ sample_kernel(const SampleParams p) {
   uint16_t* tokens = reinterpret_cast<uint16_t*>(vals + p.cap);
   static_assert(sizeof(SampleShared<NW>) % 16 == 0, "");
   const Team<NW> tm{NW == 1 ? (int)(threadIdx.x & 31) : (int)threadIdx.x, sh.red};
-  const RowLimits l = row_limits(p, r, tm.tid);
+  RowLimits l = row_limits(p, r, tm.tid);
   const int words = (p.V + 63) >> 6;
   const uint64_t* allow = LISTS ? p.allow + r * words : nullptr;
   const RowGlobal<BF16> row{reinterpret_cast<const char*>(p.logits) + r * p.ld * (BF16 ? 2 : 4), allow, p.V, p.vec, false};
@@ -1008,7 +1039,9 @@ sample_kernel(const SampleParams p) {
         return;
       }
       const RowShared list{vals, tokens, n};
-      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, Scale(l.temperature), 0.f, LeftOut<BF16>{row, 0.f}, infinite);
+      const Scale sc(l.temperature);
+      if (l.min_p > 0.f) l.least = min_p_bound(m, l.min_p, sc.t);
+      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f}, infinite);
       return;
     }
   }
