@@ -17,6 +17,7 @@
 // e^ and sums in fp64.
 #pragma once
 
+#include <type_traits>
 #include "common.cuh"
 
 namespace grace {
@@ -48,6 +49,29 @@ __device__ __forceinline__ float sample_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// What weights are and are added up in before 64 bits decide.  A warp's rows are many and short: fp32, and one in some dozens
+// is done again.  In a CTA's rows, of up to 65536 tokens, a border is next to some sum nearly always, and the one row that is done
+// again holds up the call (64 x 65472, top-p 0.95: 70 us, 28 without): fp64, with an e^ that is good to 2^-32.
+template <int NW>
+using Sum = std::conditional_t<NW == 1, float, double>;
+// 2^y for y <= 0 to 2^-32 of itself: 2^floor times the Taylor polynomial of degree 8 of 2^f, |f| <= 1/2
+// ((ln 2 / 2)^9 / 9! = 2e-10); 2^-1000 and less come out as about 2^-1000.
+__device__ __forceinline__ double sample_ex2_fine(double y) {
+  y = fmax(y, -1000.);
+  const double magic = 6755399441055744.;                  // 3 x 2^51: the sum's last bits are the nearest integer
+  const double r = y + magic, f = y - (r - magic);
+  double p = 1.3215486790144305e-6;                        // ln(2)^k / k!
+  p = fma(p, f, 1.5252733804059841e-5);
+  p = fma(p, f, 1.5403530393381606e-4);
+  p = fma(p, f, 1.3333558146428443e-3);
+  p = fma(p, f, 9.6181291076284772e-3);
+  p = fma(p, f, 5.5504108664821580e-2);
+  p = fma(p, f, 2.4022650695910072e-1);
+  p = fma(p, f, 6.9314718055994531e-1);
+  p = fma(p, f, 1.);
+  return __hiloint2double(__double2hiint(p) + (__double2loint(r) << 20), __double2loint(p));
+}
+
 // The histogram's step of a value.
 __device__ __forceinline__ int sample_bucket(float m, float x, float c) { return min(kSampleBuckets - 1, (int)((m - x) * (c * kSampleSteps))); }
 // A weight in 64 bits, for the rows that need them (a function of its own: e^ in 64 bits is long).
@@ -202,8 +226,8 @@ struct SampleShared {
   float found_t;
   uint32_t above;
   int found_all, place;
-  float above_w;
-  int len, copies, pad[1];
+  double above_w;
+  int len, copies;
 };
 
 // First step at which the histogram's running sum reaches goal(its whole sum) (sh.bucket) and the sum in front of it (sh.above);
@@ -254,15 +278,21 @@ struct Sampler {
   float m;                       // largest value
   float c;                       // log2(e) / T
   float temperature;
-  float margin;                  // of sums, relative to the whole
+  using W = Sum<NW>;
+  double c64;                    // log2(e) / T, for fp64 sums
+  W margin;                      // of sums, relative to the whole
   int group;                     // elements of a table entry
   // top-p counts elements that the list leaves out: their weight with the list's (0: the row is all there is), and where they are
-  float whole_row;
+  W whole_row;
   Rest rest;
   static constexpr int NT = NW * 32;
   static constexpr int kList = SampleShared<NW>::kList;
 
-  __device__ __forceinline__ float weight(float x) const { return sample_ex2((x - m) * c); }
+  __device__ __forceinline__ float rough(float x) const { return sample_ex2((x - m) * c); }
+  __device__ __forceinline__ W weight(float x) const {
+    if constexpr (NW == 1) return rough(x);
+    else return sample_ex2_fine(((double)x - (double)m) * c64);
+  }
   __device__ __forceinline__ double weight64(float x) const { return sample_weight64(x, m, temperature); }
   __device__ __forceinline__ int bucket_of(float x) const { return sample_bucket(m, x, c); }
   template <class F>
@@ -280,7 +310,7 @@ struct Sampler {
   __device__ __forceinline__ Cut narrow(const Cut cut, const int k, const float p, const int step, const int step_above) const {
     // fixed point: the sum of any row below 2^32
     const float scale = MASS ? __uint_as_float((uint32_t)(126 + __clz(row.n - 1)) << 23) : 1.f;   // 2^(31 - ceil(log2 n))
-    auto share = [&](float x) { return MASS ? __float2uint_rn(weight(x) * scale) : 1u; };
+    auto share = [&](float x) { return MASS ? __float2uint_rn(rough(x) * scale) : 1u; };
     tm.sync();
     if (tm.tid == 0) { shared->n_list = 0; shared->found = 0; }
     int b = step, n_above = step_above;
@@ -294,7 +324,7 @@ struct Sampler {
       find_bucket(tm, *shared, [&](uint32_t all) {
         if (!MASS) return (uint32_t)k;
         // within what the histogram holds
-        const float want = (whole_row > 0.f ? whole_row * scale : (float)all) * p;
+        const float want = (whole_row > W(0) ? (float)whole_row * scale : (float)all) * p;
         return min(max(1u, (uint32_t)fminf(want, 4294967040.f)), max(1u, all));
       });
       if (shared->bucket < 0) return cut;                  // no more than k elements
@@ -303,30 +333,44 @@ struct Sampler {
     } else {
       tm.sync();
     }
-    float whole = 0.f, above = 0.f;
-    for_each([&](float x, int place) {
-      if (!cut.keeps(x, place)) return;
-      const int at = bucket_of(x);
+    W whole = W(0), above = W(0);
+    // the step's values; fixed point may have missed the step by a little: then its neighbour's
+    for (int tries = 0; ; ++tries) {
+      whole = above = W(0);
+      W inside = W(0);
+      for_each([&](float x, int place) {
+        if (!cut.keeps(x, place)) return;
+        const int at = bucket_of(x);
+        if (MASS) {
+          const W w = weight(x);
+          whole += w;
+          above += at < b ? w : W(0);
+          if (NW > 1) inside += at == b ? w : W(0);
+        }
+        if (at == b) {
+          const int i = atomicAdd(&shared->n_list, 1);
+          if (i < kList) shared->list[i] = x;
+        }
+      });
       if (MASS) {
-        const float w = weight(x);
-        whole += w;
-        above += at < b ? w : 0.f;
+        whole = whole_row > W(0) ? whole_row : tm.sum(whole);
+        above = tm.sum(above);
       }
-      if (at == b) {
-        const int i = atomicAdd(&shared->n_list, 1);
-        if (i < kList) shared->list[i] = x;
-      }
-    });
-    if (MASS) {
-      whole = whole_row > 0.f ? whole_row : tm.sum(whole);
-      above = tm.sum(above);
+      tm.sync();
+      if (!MASS || NW == 1 || tries == 8) break;
+      inside = tm.sum(inside);
+      const int move = above > (W)p * whole ? -1 : (above + inside < (W)p * whole ? 1 : 0);
+      if (move == 0 || b + move < 0 || b + move >= kSampleBuckets) break;
+      b += move;
+      tm.sync();
+      if (tm.tid == 0) shared->n_list = 0;
+      tm.sync();
     }
-    tm.sync();
     const int n = shared->n_list;
     int len = n, copies = 1;
     if (n > kList) {
       narrow_keys<MASS>(*this, cut, k, p, b, scale, whole, above, n_above);
-      above = shared->above_w;
+      above = (W)shared->above_w;
       n_above = (int)shared->above;
       len = shared->len;
       copies = shared->copies;
@@ -336,17 +380,17 @@ struct Sampler {
       const float x = shared->list[i];
       int same = 0;
       if (MASS) {
-        float front = above;
+        W front = above;
         for (int j = 0; j < len; ++j) {
           const float y = shared->list[j];
           if (y > x) front += weight(y);
           same += y == x;
         }
         same *= copies;
-        const float w = weight(x), gap = p * whole - front, slack = margin * whole;
-        if (gap > slack && gap + slack < w * (float)same) {
-          const float q = gap / w, r = ceilf(q);
-          if (same == 1 || ((r - q) * w > slack && (q - (r - 1.f)) * w > slack)) note(x, min(same, max(1, (int)r)), same);
+        const W w = weight(x), gap = (W)p * whole - front, slack = margin * whole;
+        if (gap > slack && gap + slack < w * (W)same) {
+          const W q = gap / w, r = ceil(q);
+          if (same == 1 || ((r - q) * w > slack && (q - (r - W(1))) * w > slack)) note(x, min(same, max(1, (int)r)), same);
         }
       } else {
         int front = n_above;
@@ -403,13 +447,13 @@ struct Sampler {
   // A step with more values than the list takes: histograms of equal steps of the ordered bits, until they fit or are all the
   // same (`copies` of one list entry).
   template <bool MASS>
-  static __device__ __noinline__ void narrow_keys(const Sampler s, const Cut cut, const int k, const float p, const int b, const float scale, const float whole,
-                                                  const float above, const int n_above) {
+  static __device__ __noinline__ void narrow_keys(const Sampler s, const Cut cut, const int k, const float p, const int b, const float scale, const W whole,
+                                                  const W above, const int n_above) {
     s.template narrow_keys_<MASS>(cut, k, p, b, scale, whole, above, n_above);
   }
   template <bool MASS>
-  __device__ __forceinline__ void narrow_keys_(const Cut cut, const int k, const float p, const int b, const float scale, const float whole,
-                                               float above, int n_above) const {
+  __device__ __forceinline__ void narrow_keys_(const Cut cut, const int k, const float p, const int b, const float scale, const W whole,
+                                               W above, int n_above) const {
     uint32_t key_lo = 0xffffffffu, key_hi = 0u;
     for_each([&](float x, int place) {
       if (cut.keeps(x, place) && bucket_of(x) == b) { const uint32_t key = ordered_key(x); key_lo = min(key_lo, key); key_hi = max(key_hi, key); }
@@ -424,16 +468,16 @@ struct Sampler {
       tm.sync();
       for_each([&](float x, int place) {
         const uint32_t key = ordered_key(x);
-        if (key >= key_lo && key <= key_hi && cut.keeps(x, place)) atomicAdd(&shared->hist[(key_hi - key) >> shift], MASS ? __float2uint_rn(weight(x) * scale) : 1u);
+        if (key >= key_lo && key <= key_hi && cut.keeps(x, place)) atomicAdd(&shared->hist[(key_hi - key) >> shift], MASS ? __float2uint_rn(rough(x) * scale) : 1u);
       });
       tm.sync();
       find_bucket(tm, *shared, [&](uint32_t all) {
-        return MASS ? min((uint32_t)fminf(fmaxf((p * whole - above) * scale, 1.f), 4294967040.f), max(1u, all)) : (uint32_t)(k - n_above);
+        return MASS ? min((uint32_t)fminf(fmaxf((float)((W)p * whole - above) * scale, 1.f), 4294967040.f), max(1u, all)) : (uint32_t)(k - n_above);
       });
       const int at = max(0, shared->bucket);
       key_hi -= (uint32_t)at << shift;
       key_lo = max(key_lo, key_hi - ((1u << shift) - 1u));
-      float more = 0.f;
+      W more = W(0);
       int inside = 0, over = 0;
       for_each([&](float x, int place) {
         if (!cut.keeps(x, place)) return;
@@ -456,7 +500,7 @@ struct Sampler {
       if (i < kList) shared->list[i] = x;
     });
     if (tm.tid == 0) {
-      shared->above_w = above;
+      shared->above_w = (double)above;
       shared->above = (uint32_t)n_above;
       shared->copies = one ? n : 1;
       shared->len = one ? min(n, 1) : n;
@@ -478,7 +522,7 @@ struct Sampler {
       if (x > top) above += w;
     });
     whole = tm.sum(whole);
-    if (whole_row > 0.f) whole += rest.weight64(tm, m, temperature);
+    if (whole_row > W(0)) whole += rest.weight64(tm, m, temperature);
     above = tm.sum(above);
     const double goal = (double)p * whole;
     auto settle = [&](float x, double front, int same) {
@@ -526,22 +570,30 @@ struct Sampler {
     tm.sync();
   }
 
-  template <class F>
-  __device__ __forceinline__ F kept_weight(const Cut cut, int i) const {
-    const float x = row.at(i);
-    return cut.keeps(x, i) ? (sizeof(F) == 8 ? (F)weight64(x) : (F)weight(x)) : F(0);
+  // EXACT: in 64 bits throughout
+  template <bool EXACT>
+  using SumOf = std::conditional_t<EXACT, double, W>;
+  template <bool EXACT>
+  __device__ __forceinline__ SumOf<EXACT> kept_weight(const Cut cut, float x, int i) const {
+    if (!cut.keeps(x, i)) return 0;
+    if constexpr (EXACT) return weight64(x);
+    else return weight(x);
   }
+  template <bool EXACT>
+  __device__ __forceinline__ SumOf<EXACT> kept_weight(const Cut cut, int i) const { return kept_weight<EXACT>(cut, row.at(i), i); }
   // The table of sums of the kept weights by groups, and the threads' sums (four groups each) up to and with their own; returns
   // the whole.
-  template <class F>
-  __device__ __forceinline__ F tabulate(const Cut cut, F* table) const {
+  template <bool EXACT>
+  __device__ __forceinline__ SumOf<EXACT> tabulate(const Cut cut) const {
+    using F = SumOf<EXACT>;
+    F* const table = reinterpret_cast<F*>(shared->table);
     tm.sync();
     F s = F(0);
 #pragma unroll 1
     for (int e = 0; e < 4; ++e) {
       if (group == 1) {                                    // a short list
         const int i = 4 * tm.tid + e;
-        const F t = i < row.n ? kept_weight<F>(cut, i) : F(0);
+        const F t = i < row.n ? kept_weight<EXACT>(cut, i) : F(0);
         table[i] = t;
         s += t;
         continue;
@@ -551,8 +603,8 @@ struct Sampler {
       if constexpr (Row::kQuads) {                         // in memory: whole quads
         for (int q = i0 >> 2; q < min(i0 + group, (row.n + 3) & ~3) >> 2; ++q) {
           const float4 v = row.quad(q);
-          auto kept = [&](float x, int j) { return cut.keeps(x, 4 * q + j) ? (sizeof(F) == 8 ? (F)weight64(x) : (F)weight(x)) : F(0); };
-          t += (kept(v.x, 0) + kept(v.y, 1)) + (kept(v.z, 2) + kept(v.w, 3));
+          t += (kept_weight<EXACT>(cut, v.x, 4 * q) + kept_weight<EXACT>(cut, v.y, 4 * q + 1)) +
+               (kept_weight<EXACT>(cut, v.z, 4 * q + 2) + kept_weight<EXACT>(cut, v.w, 4 * q + 3));
         }
         table[4 * tm.tid + e] = t;
         s += t;
@@ -561,7 +613,7 @@ struct Sampler {
       // each thread from another of its elements on, round once: side by side they would all be on one bank
       int k = tm.tid % group;
       for (int i = 0; i < group; ++i) {
-        if (i0 + k < row.n) t += kept_weight<F>(cut, i0 + k);
+        if (i0 + k < row.n) t += kept_weight<EXACT>(cut, i0 + k);
         k = k + 1 == group ? 0 : k + 1;
       }
       table[4 * tm.tid + e] = t;
@@ -574,8 +626,10 @@ struct Sampler {
   }
 
   // Place of the first kept element at which the running sum exceeds u * whole; `sure` unless a border is within `slack`.
-  template <class F>
-  __device__ __forceinline__ int pick(const Cut cut, const F* table, F whole, float u, F slack, bool& sure) const {
+  template <bool EXACT>
+  __device__ __forceinline__ int pick(const Cut cut, SumOf<EXACT> whole, float u, SumOf<EXACT> slack, bool& sure) const {
+    using F = SumOf<EXACT>;
+    const F* const table = reinterpret_cast<const F*>(shared->table);
     const F* prefix = reinterpret_cast<const F*>(shared->prefix);
     const F goal = (F)u * whole;
     int lo = 0, hi = NT - 1;
@@ -591,7 +645,7 @@ struct Sampler {
       const F s = table[e];
       if (run + s <= goal && e + 1 < 4 * NT && (e + 1) * group < row.n) { run += s; continue; }
       for (int i = e * group; i < min((e + 1) * group, row.n); ++i) {
-        const F w = kept_weight<F>(cut, i);
+        const F w = kept_weight<EXACT>(cut, i);
         if (w > F(0)) {
           last = i;
           if (run + w > goal) { sure = goal - run > slack && run + w - goal > slack; return i; }
@@ -601,20 +655,21 @@ struct Sampler {
     }
     // u next to 1: the last kept element with a weight
     for (int i = row.n - 1; i >= 0 && last < 0; --i)
-      if (kept_weight<F>(cut, i) > F(0)) last = i;
+      if (kept_weight<EXACT>(cut, i) > F(0)) last = i;
     return last;
   }
   // A draw by sums in 64 bits, for the threads that are not sure (`mine`); `build`: the table does not hold them yet.
   static __device__ __noinline__ int place64(const Sampler s, const Cut cut, const float u, const bool mine, const bool build, const int place) {
-    const double whole = build ? s.template tabulate<double>(cut, s.shared->table) : s.shared->prefix[NT - 1];
+    const double whole = build ? s.template tabulate<true>(cut) : s.shared->prefix[NT - 1];
     bool ignored;
-    return mine ? s.template pick<double>(cut, s.shared->table, whole, u, 0., ignored) : place;
+    return mine ? s.template pick<true>(cut, whole, u, 0., ignored) : place;
   }
   // The same by a whole warp for one draw (all lanes return it): the lanes take a group's elements at once.
-  __device__ __forceinline__ int pick_together(const Cut cut, const float* table, float whole, float u, float slack, bool& sure) const {
-    const float* prefix = reinterpret_cast<const float*>(shared->prefix);
+  __device__ __forceinline__ int pick_together(const Cut cut, W whole, float u, W slack, bool& sure) const {
+    const W* const prefix = reinterpret_cast<const W*>(shared->prefix);
+    const W* const table = reinterpret_cast<const W*>(shared->table);
     const int lane = tm.tid & 31;
-    const float goal = u * whole;
+    const W goal = (W)u * whole;
     int lo = 0;
     if (NW == 1) {
       const uint32_t over = __ballot_sync(kFullMask, prefix[lane] > goal);
@@ -626,25 +681,24 @@ struct Sampler {
         if (prefix[mid] > goal) hi = mid; else lo = mid + 1;
       }
     }
-    float run = lo > 0 ? prefix[lo - 1] : 0.f;
-    const float4 t = reinterpret_cast<const float4*>(table)[lo];
+    W run = lo > 0 ? prefix[lo - 1] : W(0);
     int e = 4 * lo;
-    if (run + t.x <= goal) { run += t.x; ++e; if (run + t.y <= goal) { run += t.y; ++e; if (run + t.z <= goal) { run += t.z; ++e; } } }
+    while (e < 4 * lo + 3 && run + table[e] <= goal) run += table[e++];
     sure = false;
     for (int i0 = e * group; i0 < min((e + 1) * group, row.n); i0 += 32) {
       const int i = i0 + lane;
-      const float w = i < min((e + 1) * group, row.n) ? kept_weight<float>(cut, i) : 0.f;
-      float upto = w;
+      const W w = i < min((e + 1) * group, row.n) ? kept_weight<false>(cut, i) : W(0);
+      W upto = w;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const float v = __shfl_up_sync(kFullMask, upto, o);
+        const W v = __shfl_up_sync(kFullMask, upto, o);
         if (lane >= o) upto += v;
       }
       upto += run;
-      const uint32_t over = __ballot_sync(kFullMask, w > 0.f && upto > goal);
+      const uint32_t over = __ballot_sync(kFullMask, w > W(0) && upto > goal);
       if (over != 0u) {
         const int at = __ffs(over) - 1;
-        const float after = __shfl_sync(kFullMask, upto, at), own = __shfl_sync(kFullMask, w, at);
+        const W after = __shfl_sync(kFullMask, upto, at), own = __shfl_sync(kFullMask, w, at);
         sure = goal - (after - own) > slack && after - goal > slack;
         return i0 + at;
       }
@@ -700,22 +754,21 @@ __device__ __forceinline__ void store_all(const SampleParams& p, const RowLimits
 // The limits exactly, on a row that holds all elements they can keep, and the draws.  m: the largest value (finite).
 template <int NW, bool BF16, class Row>
 __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row& row, const Team<NW>& tm, SampleShared<NW>& sh, int64_t r, float m,
-                                               const RowLimits& l, const Scale& sc, float whole_row, const LeftOut<BF16>& rest, bool infinite) {
+                                               const RowLimits& l, const Scale& sc, Sum<NW> whole_row, const LeftOut<BF16>& rest, bool infinite) {
   constexpr int NT = NW * 32;
   using S = Sampler<NW, Row, LeftOut<BF16>>;
   // Sums' worst error, relative to the whole.  A weight's: its exponent's, 3.5 x 2^-24 of z = (max - x) / T (the difference, c, the
   // product), whose mean over the weights is at most ln V (a distribution's entropy is); 2^-22 of ex2.  A sum's: 2^-24 for each of
-  // the 30 additions that an addend passes at most.  V 2048: 3.3e-6, V 65536: 4.4e-6.
-  const float margin = p.V > 2048 ? 4.5e-6f : 3.4e-6f;
+  // the 30 additions that an addend passes at most: 3.3e-6 for V = 2048.  In fp64: 2^-32 of a weight's, the rest below 2^-45.
+  const Sum<NW> margin = NW == 1 ? Sum<NW>(3.4e-6) : Sum<NW>(1e-9);
   const int group = (row.n + 4 * NT - 1) / (4 * NT);
-  const S s{row, tm, &sh, m, sc.c, sc.t, margin, Row::kQuads ? (group + 3) & ~3 : group, whole_row, rest};
+  const S s{row, tm, &sh, m, sc.c, sc.t, NW == 1 ? 0. : 1.4426950408889634 / (double)sc.t, margin, Row::kQuads ? (group + 3) & ~3 : group, whole_row, rest};
   Cut cut = {-INFINITY, -1};
   if (l.top_k > 0 && l.top_k < row.n) cut = s.template narrow<false>(cut, l.top_k, 0.f, l.step, l.step_above);
   if (l.top_p < 1.f) cut = s.template narrow<true>(cut, 0, fmaxf(l.top_p, 0.f), -1, 0);
   if (l.least > cut.t) cut = Cut{l.least, 0x7fffffff};
-  float* table32 = reinterpret_cast<float*>(sh.table);
-  const float whole = s.template tabulate<float>(cut, table32);
-  const float log_whole = logf(whole);
+  const Sum<NW> whole = s.template tabulate<false>(cut);
+  const float log_whole = logf((float)whole);
   auto store = [&](int d, int place) {
     place = max(place, 0);
     const float x = row.at(place);
@@ -732,8 +785,7 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
     bool sure = false;
     int place = -1;
     if (!have64 && in) {
-      place = together ? s.pick_together(cut, table32, whole, u, s.margin * whole, sure)
-                       : s.template pick<float>(cut, table32, whole, u, s.margin * whole, sure);
+      place = together ? s.pick_together(cut, whole, u, s.margin * whole, sure) : s.template pick<false>(cut, whole, u, s.margin * whole, sure);
     }
     const int doubt = tm.reduce(in && !sure ? 1 : 0, [](int a, int e) { return a | e; });
     if (doubt) {
@@ -819,7 +871,7 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   const bool by_count = l.top_k > 0 && l.top_k < n, by_mass = !by_count && l.top_p < 1.f;
   if (l.min_p > 0.f) l.least = min_p_bound(m, l.min_p, sc.t);
   float bound = by_count && l.top_p < 1.f ? -INFINITY : l.least;
-  float whole_row = 0.f;
+  Sum<NW> whole_row = 0;
   if (by_count) {
     clear_hist(tm, sh);
     tm.sync();
@@ -839,15 +891,19 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
     if (l.step >= 0 && l.step < kSampleBuckets - 1)
       bound = fmaxf(bound, m - ((float)(l.step + 1) * 1.0001f) / (sc.c * kSampleSteps) - fabsf(m) * 0x1p-20f);
   } else if (by_mass) {
-    float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
-#pragma unroll 4
+    Sum<NW> s0 = 0, s1 = 0, s2 = 0, s3 = 0;
+    const double c64 = NW == 1 ? 0. : 1.4426950408889634 / (double)sc.t;
+    auto weight = [&](float x) -> Sum<NW> {
+      if constexpr (NW == 1) return sample_ex2((x - m) * sc.c);
+      else return sample_ex2_fine(((double)x - (double)m) * c64);
+    };
+#pragma unroll (NW == 1 ? 4 : 2)
     for (int i = 0; i < iters; ++i) {
       const float4 t = quad(first + 32 * i);
-      s0 += sample_ex2((t.x - m) * sc.c); s1 += sample_ex2((t.y - m) * sc.c);
-      s2 += sample_ex2((t.z - m) * sc.c); s3 += sample_ex2((t.w - m) * sc.c);
+      s0 += weight(t.x); s1 += weight(t.y); s2 += weight(t.z); s3 += weight(t.w);
     }
     whole_row = tm.sum((s0 + s1) + (s2 + s3));
-    const float light = (1.f - fmaxf(l.top_p, 0.f)) * whole_row / (float)n * 0.999f;
+    const float light = (1.f - fmaxf(l.top_p, 0.f)) * (float)whole_row / (float)n * 0.999f;
     bound = fmaxf(bound, m + log2f(light) / sc.c - 1e-4f / sc.c - fabsf(m) * 0x1p-20f);
   }
   if (by_count || by_mass || l.min_p > 0.f) {
@@ -952,9 +1008,9 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
     }
     tm.sync();
     const RowShared all{vals, nullptr, p.V};
-    limit_and_draw<NW, BF16>(p, all, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f}, row.inf);
+    limit_and_draw<NW, BF16>(p, all, tm, sh, r, m, l, sc, Sum<NW>(0), LeftOut<BF16>{row, 0.f}, row.inf);
   } else if constexpr (!SHARED) {
-    limit_and_draw<NW, BF16>(p, row, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f}, row.inf);
+    limit_and_draw<NW, BF16>(p, row, tm, sh, r, m, l, sc, Sum<NW>(0), LeftOut<BF16>{row, 0.f}, row.inf);
   }
 }
 
@@ -1041,7 +1097,7 @@ sample_kernel(const SampleParams p) {
       const RowShared list{vals, tokens, n};
       const Scale sc(l.temperature);
       if (l.min_p > 0.f) l.least = min_p_bound(m, l.min_p, sc.t);
-      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, sc, 0.f, LeftOut<BF16>{row, 0.f}, infinite);
+      limit_and_draw<NW, BF16>(p, list, tm, sh, r, m, l, sc, Sum<NW>(0), LeftOut<BF16>{row, 0.f}, infinite);
       return;
     }
   }
