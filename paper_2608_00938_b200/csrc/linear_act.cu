@@ -330,6 +330,9 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 // registers one step ahead, from there into the 2 KB, and a thread adds its row's where the results will lie.  No warp waits
 // for another.  WIDE: rows of y and of the residual start on 16 bytes; otherwise the warp moves single elements between the
 // 2 KB and memory.
+// LONG (fp32 results of more than 16 k-blocks): the tensor cores' accumulator drops what it cannot hold at every step, towards
+// zero, and over 512 steps that adds up to 5e-6 of the result.  So an accumulator takes 16 k-blocks, and the epilogue's warps
+// add them up in registers, rounded to nearest.
 // (Eight warps in two groups that share a buffer and its barriers: 84 us for 65536 x 2048 x 512 in e4m3, without activation.)
 // ---------------------------------------------------------------------------------------------
 constexpr int kAPStages = 5;
@@ -340,6 +343,7 @@ constexpr int kAPTurn = 32 * kAPRow;
 constexpr int kAPCols = 2 * kAPWarpCols * 4;               // scales and biases of the warp's columns
 constexpr int kAPSmem = kAPStages * kAPStageBytes + kAPWarps * (kAPTurn + kAPCols) + 256;
 constexpr int kAPThreads = 64 + 32 * kAPWarps;
+constexpr int kAPSegment = 16;                             // k-blocks that LONG leaves to one accumulator
 static_assert(kAPSmem >= tc::kTmemAllSmem && kAPSmem <= 227 * 1024, "");
 
 // v = acc * xs * scale + bias of N columns, whose scales and biases (kAPWarpCols behind the scales) lie in shared memory.
@@ -363,7 +367,7 @@ __device__ __forceinline__ void act_affine(float (&v)[N], const uint32_t (&acc)[
   }
 }
 
-template <bool F8, bool F32, bool WIDE>
+template <bool F8, bool F32, bool WIDE, bool LONG>
 __global__ void __launch_bounds__(kAPThreads, 1)
 act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
                 const __grid_constant__ CUtensorMap map_y, const ActParams p) {
@@ -424,26 +428,30 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     if (lane == 0 && rank == 0) {                           // ---- even CTA: MMA issuer for the pair ----
       const uint32_t idesc = act_idesc<F8>(256, p.bn);
       int it = 0, local = 0;
-      for (int tile = pair; tile < total; tile += n_pairs, ++local) {
-        const int ab = local & 1;
-        if (!tc::mbar_wait_cluster(acc_empty + ab, ((local >> 1) & 1) ^ 1, abort_flag)) break;
-        tc::tc_fence_after();
-        const uint32_t d_tmem = tmem_base + (uint32_t)(ab * 256);
+      for (int tile = pair; tile < total; tile += n_pairs) {
         bool ok = true;
-        for (int kb = 0; kb < p.KB; ++kb, ++it) {
-          const int s = it % kAPStages;
-          if (!tc::mbar_wait_cluster(full + s, (it / kAPStages) & 1, abort_flag)) { ok = false; break; }
+        for (int kb0 = 0; ok && kb0 < p.KB; kb0 += LONG ? kAPSegment : p.KB, ++local) {
+          const int ab = local & 1, kb1 = LONG ? min(kb0 + kAPSegment, p.KB) : p.KB;
+          ok = tc::mbar_wait_cluster(acc_empty + ab, ((local >> 1) & 1) ^ 1, abort_flag);
+          if (!ok) break;
           tc::tc_fence_after();
-          const uint32_t a_addr = tc::smem_addr(tiles + s * kAPStageBytes);
-          const uint64_t a_desc = tc::smem_desc_sw128(a_addr, 16, 1024);
-          const uint64_t b_desc = tc::smem_desc_sw128(a_addr + 128 * 128, 16, 1024);
+          const uint32_t d_tmem = tmem_base + (uint32_t)(ab * 256);
+          for (int kb = kb0; kb < kb1; ++kb, ++it) {
+            const int s = it % kAPStages;
+            ok = tc::mbar_wait_cluster(full + s, (it / kAPStages) & 1, abort_flag);
+            if (!ok) break;
+            tc::tc_fence_after();
+            const uint32_t a_addr = tc::smem_addr(tiles + s * kAPStageBytes);
+            const uint64_t a_desc = tc::smem_desc_sw128(a_addr, 16, 1024);
+            const uint64_t b_desc = tc::smem_desc_sw128(a_addr + 128 * 128, 16, 1024);
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            act_mma<F8, true>(d_tmem, a_desc + (uint64_t)(2 * k), b_desc + (uint64_t)(2 * k), idesc, (kb | k) ? 1u : 0u);
-          tc::mma_commit_pair(empty + s, 3);
+            for (int k = 0; k < 4; ++k)
+              act_mma<F8, true>(d_tmem, a_desc + (uint64_t)(2 * k), b_desc + (uint64_t)(2 * k), idesc, (kb > kb0 || k) ? 1u : 0u);
+            tc::mma_commit_pair(empty + s, 3);
+          }
+          if (ok) tc::mma_commit_pair(acc_full + ab, 3);
         }
         if (!ok) break;
-        tc::mma_commit_pair(acc_full + ab, 3);
       }
     }
   } else {
@@ -498,13 +506,12 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     int m0 = tile_m * 256 + (int)rank * 128 + q * 32, n0 = tile_n * p.bn + col;
     fetch(m0, n0);
     int local = 0;
-    for (int tile = pair; tile < total; tile += n_pairs, ++local) {
+    for (int tile = pair; tile < total; tile += n_pairs) {
       m0 = tile_m * 256 + (int)rank * 128 + q * 32;
       n0 = tile_n * p.bn + col;
       tile_m += step_m;
       tile_n += step_n;
       if (tile_n >= n_tiles) { tile_n -= n_tiles; ++tile_m; }
-      const int ab = local & 1;
       if (WIDE && p.residual != nullptr) hold(m0, n0);
       const float xs = xs_next;
       __syncwarp();                                         // the tile in front has been finished with them
@@ -514,25 +521,9 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         scale[kAPWarpCols + 32 * i + lane] = bias_next[i];
       }
       fetch(tile_m * 256 + (int)rank * 128 + q * 32, tile_n * p.bn + col);
-      bool ok = tc::mbar_wait_cluster(acc_full + ab, (local >> 1) & 1, abort_flag);
-      ok = __all_sync(kFullMask, ok);
-      if (!ok) break;
-      tc::tc_fence_after();
-      const uint32_t t_acc = tmem_base + (uint32_t)(ab * 256 + col) + ((uint32_t)(q * 32) << 16);
-#pragma unroll 1
-      for (int c0 = 0; c0 < kAPWarpCols; c0 += kCols) {
-        uint32_t r[kCols];
-        if constexpr (F32) tc::tmem_ld16(t_acc + c0, r); else tc::tmem_ld32(t_acc + c0, r);
-        tc::tmem_ld_wait();
-        if (c0 + kCols == kAPWarpCols) {                             // this part of the accumulator has been read
-          tc::tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            if (rank == 0) tc::mbar_arrive(acc_empty + ab);
-            else tc::mbar_arrive_remote(acc_empty + ab, 0);
-          }
-        }
-        if (m0 >= p.M || n0 + c0 >= p.N || col + c0 >= p.bn) continue;             // the same for the whole warp
+      // the finished columns c0 .. of the tile: scales, bias, activation, residual, and out
+      auto finish = [&](const int c0, const uint32_t (&r)[kCols]) {
+        if (m0 >= p.M || n0 + c0 >= p.N || col + c0 >= p.bn) return;               // the same for the whole warp
         float v[kCols];
         act_affine<F8>(v, r, xs, scale + c0);
         act_all<F32>(v, p.act);
@@ -593,6 +584,55 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
             }
           }
         }
+      };
+      // the accumulator: waits for it (false: it will not come), and gives it back
+      auto wait_full = [&]() {
+        bool ok = tc::mbar_wait_cluster(acc_full + (local & 1), (local >> 1) & 1, abort_flag);
+        ok = __all_sync(kFullMask, ok);
+        tc::tc_fence_after();
+        return ok;
+      };
+      auto give_back = [&]() {
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (rank == 0) tc::mbar_arrive(acc_empty + (local & 1));
+          else tc::mbar_arrive_remote(acc_empty + (local & 1), 0);
+        }
+        ++local;
+      };
+      auto t_acc = [&]() { return tmem_base + (uint32_t)((local & 1) * 256 + col) + ((uint32_t)(q * 32) << 16); };
+      bool ok = true;
+      if constexpr (LONG) {
+        float sum[kAPWarpCols / kCols][kCols];
+        for (int kb0 = 0; kb0 < p.KB; kb0 += kAPSegment) {
+          ok = wait_full();
+          if (!ok) break;
+#pragma unroll
+          for (int c = 0; c < kAPWarpCols / kCols; ++c) {
+            uint32_t r[kCols];
+            tc::tmem_ld16(t_acc() + c * kCols, r);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) sum[c][i] = kb0 == 0 ? __uint_as_float(r[i]) : sum[c][i] + __uint_as_float(r[i]);
+          }
+          give_back();
+        }
+        if (!ok) break;
+#pragma unroll
+        for (int c = 0; c < kAPWarpCols / kCols; ++c) finish(c * kCols, reinterpret_cast<const uint32_t (&)[kCols]>(sum[c]));
+      } else {
+        ok = wait_full();
+        if (!ok) break;
+        const uint32_t t = t_acc();
+#pragma unroll 1
+        for (int c0 = 0; c0 < kAPWarpCols; c0 += kCols) {
+          uint32_t r[kCols];
+          if constexpr (F32) tc::tmem_ld16(t + c0, r); else tc::tmem_ld32(t + c0, r);
+          tc::tmem_ld_wait();
+          if (c0 + kCols == kAPWarpCols) give_back();       // this part of the accumulator has been read
+          finish(c0, r);
+        }
       }
     }
     if (WIDE && lane == 0) tc::bulk_wait_all();
@@ -627,7 +667,7 @@ static grace_status_t launch_act(const CUtensorMap& mx, const CUtensorMap& mw, c
   return GRACE_OK;
 }
 
-template <bool F8, bool F32, bool WIDE>
+template <bool F8, bool F32, bool WIDE, bool LONG = false>
 static grace_status_t launch_act_pair(const CUtensorMap& mx, const CUtensorMap& mw, const CUtensorMap& my, const ActParams& p, cudaStream_t s) {
   static unsigned long long attr_set_devices = 0;
   static int max_clusters_of[kMaxDevices] = {0};
@@ -640,11 +680,11 @@ static grace_status_t launch_act_pair(const CUtensorMap& mx, const CUtensorMap& 
   cfg.blockDim = dim3(kAPThreads); cfg.dynamicSmemBytes = kAPSmem; cfg.stream = s; cfg.attrs = attr; cfg.numAttrs = 2;
   DeviceSetup su(&attr_set_devices);
   if (su) {
-    GRACE_CUDA_TRY(cudaFuncSetAttribute(act_pair_kernel<F8, F32, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAPSmem));
+    GRACE_CUDA_TRY(cudaFuncSetAttribute(act_pair_kernel<F8, F32, WIDE, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize, kAPSmem));
     int n_sm = 0, clusters = 0;
     GRACE_CUDA_TRY(cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, su.dev));
     cfg.gridDim = dim3(n_sm & ~1);
-    GRACE_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, act_pair_kernel<F8, F32, WIDE>, &cfg));
+    GRACE_CUDA_TRY(cudaOccupancyMaxActiveClusters(&clusters, act_pair_kernel<F8, F32, WIDE, LONG>, &cfg));
     if (clusters <= 0) return GRACE_CUDA_ERROR;
     max_clusters_of[su.dev] = clusters < n_sm / 2 ? clusters : n_sm / 2;
     su.done();
@@ -652,7 +692,7 @@ static grace_status_t launch_act_pair(const CUtensorMap& mx, const CUtensorMap& 
   const int64_t total = (int64_t)((p.N + p.bn - 1) / p.bn) * ((p.M + 255) / 256);
   const int most = max_clusters_of[su.dev];
   cfg.gridDim = dim3(2 * (unsigned)(total < most ? total : most));
-  GRACE_CUDA_TRY(cudaLaunchKernelEx(&cfg, act_pair_kernel<F8, F32, WIDE>, mx, mw, my, p));
+  GRACE_CUDA_TRY(cudaLaunchKernelEx(&cfg, act_pair_kernel<F8, F32, WIDE, LONG>, mx, mw, my, p));
   GRACE_LAUNCH_CHECK();
   return GRACE_OK;
 }
@@ -726,6 +766,8 @@ static grace_status_t linear_act_impl(const void* x, int64_t ldx, const float* x
   if (wide && !tc::make_tmap_typed(&my, y, 2, dy, sy, by, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, size,
                                    CU_TENSOR_MAP_SWIZZLE_64B))
     return GRACE_CUDA_ERROR;
+  if (f32 && p.KB > kAPSegment)
+    return wide ? launch_act_pair<F8, true, true, true>(mx, mw, my, p, s) : launch_act_pair<F8, true, false, true>(mx, mw, my, p, s);
   if (f32) return wide ? launch_act_pair<F8, true, true>(mx, mw, my, p, s) : launch_act_pair<F8, true, false>(mx, mw, my, p, s);
   return wide ? launch_act_pair<F8, false, true>(mx, mw, my, p, s) : launch_act_pair<F8, false, false>(mx, mw, my, p, s);
 }
