@@ -332,7 +332,7 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 // 2 KB and memory.
 // LONG (fp32 results of more than 16 k-blocks): the tensor cores' accumulator drops what it cannot hold at every step, towards
 // zero, and over 512 steps that adds up to 5e-6 of the result.  So an accumulator takes 16 k-blocks, and the epilogue's warps
-// add them up in registers, rounded to nearest.
+// add them up in registers, rounded to nearest, while the other accumulator fills.
 // (Eight warps in two groups that share a buffer and its barriers: 84 us for 65536 x 2048 x 512 in e4m3, without activation.)
 // ---------------------------------------------------------------------------------------------
 constexpr int kAPStages = 5;
@@ -343,7 +343,9 @@ constexpr int kAPTurn = 32 * kAPRow;
 constexpr int kAPCols = 2 * kAPWarpCols * 4;               // scales and biases of the warp's columns
 constexpr int kAPSmem = kAPStages * kAPStageBytes + kAPWarps * (kAPTurn + kAPCols) + 256;
 constexpr int kAPThreads = 64 + 32 * kAPWarps;
-constexpr int kAPSegment = 16;                             // k-blocks that LONG leaves to one accumulator
+// k-blocks that LONG leaves to one accumulator; a tile's first, during which the tile in front is finished, has twice as many
+constexpr int kAPSegment = 16;
+__device__ __forceinline__ int act_segment_end(int kb) { return kb + (kb == 0 ? 2 * kAPSegment : kAPSegment); }
 static_assert(kAPSmem >= tc::kTmemAllSmem && kAPSmem <= 227 * 1024, "");
 
 // v = acc * xs * scale + bias of N columns, whose scales and biases (kAPWarpCols behind the scales) lie in shared memory.
@@ -430,8 +432,9 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       int it = 0, local = 0;
       for (int tile = pair; tile < total; tile += n_pairs) {
         bool ok = true;
-        for (int kb0 = 0; ok && kb0 < p.KB; kb0 += LONG ? kAPSegment : p.KB, ++local) {
-          const int ab = local & 1, kb1 = LONG ? min(kb0 + kAPSegment, p.KB) : p.KB;
+        for (int kb0 = 0, kb1; ok && kb0 < p.KB; kb0 = kb1, ++local) {
+          const int ab = local & 1;
+          kb1 = LONG ? min(act_segment_end(kb0), p.KB) : p.KB;
           ok = tc::mbar_wait_cluster(acc_empty + ab, ((local >> 1) & 1) ^ 1, abort_flag);
           if (!ok) break;
           tc::tc_fence_after();
@@ -488,30 +491,77 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
     // the row's scale and the columns' vectors, one tile ahead; the latter in a copy of the warp's own
     float* const scale = reinterpret_cast<float*>(turns + kAPWarps * kAPTurn + (warp - 2) * kAPCols);
     constexpr int kVec = kAPWarpCols / 32;
-    float xs_next = 1.f, ws_next[kVec], bias_next[kVec];
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) { ws_next[i] = 1.f; bias_next[i] = 0.f; }
+    float xs_next, ws_next[kVec], bias_next[kVec];
     auto fetch = [&](int m0, int n0) {
-      if (F8 && p.x_scale != nullptr) xs_next = __ldg(p.x_scale + min(m0 + lane, p.M - 1));
+      xs_next = F8 && p.x_scale != nullptr ? __ldg(p.x_scale + min(m0 + lane, p.M - 1)) : 1.f;
 #pragma unroll
       for (int i = 0; i < kVec; ++i) {
         const int n = min(n0 + 32 * i + lane, p.N - 1);
-        if (F8 && p.w_scale != nullptr) ws_next[i] = __ldg(p.w_scale + n);
-        if (p.bias != nullptr) bias_next[i] = __ldg(p.bias + n);
+        ws_next[i] = F8 && p.w_scale != nullptr ? __ldg(p.w_scale + n) : 1.f;
+        bias_next[i] = p.bias != nullptr ? __ldg(p.bias + n) : 0.f;
       }
     };
+    int local = 0;                                          // accumulators so far
+    // the accumulator: waits for it (false: it will not come), and gives it back
+    auto wait_full = [&]() {
+      bool ok = tc::mbar_wait_cluster(acc_full + (local & 1), (local >> 1) & 1, abort_flag);
+      ok = __all_sync(kFullMask, ok);
+      tc::tc_fence_after();
+      return ok;
+    };
+    auto give_back = [&]() {
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (rank == 0) tc::mbar_arrive(acc_empty + (local & 1));
+        else tc::mbar_arrive_remote(acc_empty + (local & 1), 0);
+      }
+      ++local;
+    };
+    auto t_acc = [&]() { return tmem_base + (uint32_t)((local & 1) * 256 + col) + ((uint32_t)(q * 32) << 16); };
     // the next tile's coordinates without a division
     const int step_m = n_pairs / n_tiles, step_n = n_pairs % n_tiles;
     int tile_m = pair / n_tiles, tile_n = pair % n_tiles;
     int m0 = tile_m * 256 + (int)rank * 128 + q * 32, n0 = tile_n * p.bn + col;
-    fetch(m0, n0);
-    int local = 0;
+    if (!LONG) fetch(m0, n0);
     for (int tile = pair; tile < total; tile += n_pairs) {
-      m0 = tile_m * 256 + (int)rank * 128 + q * 32;
-      n0 = tile_n * p.bn + col;
-      tile_m += step_m;
-      tile_n += step_n;
-      if (tile_n >= n_tiles) { tile_n -= n_tiles; ++tile_m; }
+      if constexpr (LONG) {
+        // All segments but the last into registers; with the last they go back into its accumulator, and on as one.  (64 of a
+        // thread's 96 registers: nothing of the finish is fetched ahead, and the accumulator is read by eights.  What does not fit
+        // goes to the L2 and back, the shared memory having left no L1: 13 us a tile.)
+        float sum[kAPWarpCols / 8][8];
+        bool ok = true;
+        for (int kb0 = 0; kb0 < p.KB; kb0 = act_segment_end(kb0)) {
+          ok = wait_full();
+          if (!ok) break;
+          const uint32_t t = t_acc();
+          const bool last = act_segment_end(kb0) >= p.KB;
+#pragma unroll
+          for (int c = 0; c < kAPWarpCols / 8; ++c) {
+            uint32_t r[8];
+            tc::tmem_ld8(t + c * 8, r);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              sum[c][i] = kb0 == 0 ? __uint_as_float(r[i]) : sum[c][i] + __uint_as_float(r[i]);
+              r[i] = __float_as_uint(sum[c][i]);
+            }
+            if (last) tc::tmem_st8(t + c * 8, r);
+          }
+          if (!last) give_back();
+        }
+        if (!ok) break;
+        tc::tmem_st_wait();
+        m0 = tile / n_tiles * 256 + (int)rank * 128 + q * 32;
+        n0 = tile % n_tiles * p.bn + col;
+        fetch(m0, n0);
+      } else {
+        m0 = tile_m * 256 + (int)rank * 128 + q * 32;
+        n0 = tile_n * p.bn + col;
+        tile_m += step_m;
+        tile_n += step_n;
+        if (tile_n >= n_tiles) { tile_n -= n_tiles; ++tile_m; }
+      }
       if (WIDE && p.residual != nullptr) hold(m0, n0);
       const float xs = xs_next;
       __syncwarp();                                         // the tile in front has been finished with them
@@ -520,7 +570,7 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         if (F8) scale[32 * i + lane] = ws_next[i];
         scale[kAPWarpCols + 32 * i + lane] = bias_next[i];
       }
-      fetch(tile_m * 256 + (int)rank * 128 + q * 32, tile_n * p.bn + col);
+      if (!LONG) fetch(tile_m * 256 + (int)rank * 128 + q * 32, tile_n * p.bn + col);
       // the finished columns c0 .. of the tile: scales, bias, activation, residual, and out
       auto finish = [&](const int c0, const uint32_t (&r)[kCols]) {
         if (m0 >= p.M || n0 + c0 >= p.N || col + c0 >= p.bn) return;               // the same for the whole warp
@@ -585,54 +635,15 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
           }
         }
       };
-      // the accumulator: waits for it (false: it will not come), and gives it back
-      auto wait_full = [&]() {
-        bool ok = tc::mbar_wait_cluster(acc_full + (local & 1), (local >> 1) & 1, abort_flag);
-        ok = __all_sync(kFullMask, ok);
-        tc::tc_fence_after();
-        return ok;
-      };
-      auto give_back = [&]() {
-        tc::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if (rank == 0) tc::mbar_arrive(acc_empty + (local & 1));
-          else tc::mbar_arrive_remote(acc_empty + (local & 1), 0);
-        }
-        ++local;
-      };
-      auto t_acc = [&]() { return tmem_base + (uint32_t)((local & 1) * 256 + col) + ((uint32_t)(q * 32) << 16); };
-      bool ok = true;
-      if constexpr (LONG) {
-        float sum[kAPWarpCols / kCols][kCols];
-        for (int kb0 = 0; kb0 < p.KB; kb0 += kAPSegment) {
-          ok = wait_full();
-          if (!ok) break;
-#pragma unroll
-          for (int c = 0; c < kAPWarpCols / kCols; ++c) {
-            uint32_t r[kCols];
-            tc::tmem_ld16(t_acc() + c * kCols, r);
-            tc::tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < kCols; ++i) sum[c][i] = kb0 == 0 ? __uint_as_float(r[i]) : sum[c][i] + __uint_as_float(r[i]);
-          }
-          give_back();
-        }
-        if (!ok) break;
-#pragma unroll
-        for (int c = 0; c < kAPWarpCols / kCols; ++c) finish(c * kCols, reinterpret_cast<const uint32_t (&)[kCols]>(sum[c]));
-      } else {
-        ok = wait_full();
-        if (!ok) break;
-        const uint32_t t = t_acc();
+      if (!LONG && !wait_full()) break;
+      const uint32_t t = t_acc();
 #pragma unroll 1
-        for (int c0 = 0; c0 < kAPWarpCols; c0 += kCols) {
-          uint32_t r[kCols];
-          if constexpr (F32) tc::tmem_ld16(t + c0, r); else tc::tmem_ld32(t + c0, r);
-          tc::tmem_ld_wait();
-          if (c0 + kCols == kAPWarpCols) give_back();       // this part of the accumulator has been read
-          finish(c0, r);
-        }
+      for (int c0 = 0; c0 < kAPWarpCols; c0 += kCols) {
+        uint32_t r[kCols];
+        if constexpr (F32) tc::tmem_ld16(t + c0, r); else tc::tmem_ld32(t + c0, r);
+        tc::tmem_ld_wait();
+        if (c0 + kCols == kAPWarpCols) give_back();         // this part of the accumulator has been read
+        finish(c0, r);
       }
     }
     if (WIDE && lane == 0) tc::bulk_wait_all();
