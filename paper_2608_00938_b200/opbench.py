@@ -6,6 +6,9 @@ Meant for profiler captures of a single kernel on a small case and for quick sha
     python -m paper_2608_00938_b200.opbench cross_attn --B 16 --M 2048 --T 1024 --iters 5
     python -m paper_2608_00938_b200.opbench self_attn --B 32 --M 2048 --t 3
     python -m paper_2608_00938_b200.opbench topk --B 32 --M 2048 --V 1024 --K 2048
+    python -m paper_2608_00938_b200.opbench rms_norm --B 32 --M 2048 --K 512 --e4m3 --residual
+    python -m paper_2608_00938_b200.opbench linear_act --M 65536 --N 2048 --K 512 --e4m3 --act gelu
+    python -m paper_2608_00938_b200.opbench sample --B 32 --M 2048 --V 2048 --topp 0.9 --density 0.05
 """
 from __future__ import annotations
 
@@ -31,7 +34,8 @@ def _time(fn, iters, warm=2):
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("op", choices=["linear", "cross_attn", "self_attn", "topk", "mask", "lookup", "layer_norm", "log_softmax", "row_stats"])
+    ap.add_argument("op", choices=["linear", "cross_attn", "self_attn", "topk", "mask", "lookup", "layer_norm", "log_softmax", "row_stats",
+                                   "rms_norm", "linear_act", "sample"])
     for name, default in (("B", 32), ("M", 2048), ("N", 2048), ("K", 512), ("T", 1024), ("H", 8), ("d", 64),
                           ("V", 1024), ("t", 3), ("iters", 5)):
         ap.add_argument(f"--{name}", type=int, default=default)
@@ -51,6 +55,13 @@ def main():
                     help="self_attn: the cache slabs are the steps' QKV projections (nothing written but the output)")
     ap.add_argument("--folded", action="store_true",
                     help="linear: LayerNorm folded into the epilogue (row pair + column bias; centred rows)")
+    ap.add_argument("--e4m3", action="store_true", help="rms_norm: 8-bit output with row scales; linear_act: 8-bit operands with scales")
+    ap.add_argument("--act", default="none", choices=sorted(api.ACTIVATIONS), help="linear_act")
+    ap.add_argument("--temperature", type=float, default=1.0, help="sample")
+    ap.add_argument("--topk", type=int, default=0, help="sample")
+    ap.add_argument("--topp", type=float, default=1.0, help="sample")
+    ap.add_argument("--minp", type=float, default=0.0, help="sample")
+    ap.add_argument("--draws", type=int, default=1, help="sample: tokens of a row (--density: fraction of allowed tokens; 1 = no mask)")
     a = ap.parse_args()
     dev = "cuda:0"
     torch.manual_seed(0)
@@ -76,6 +87,40 @@ def main():
         else:
             us = _time(lambda: api.grace_linear(x, w, y, y if a.residual else None, a.relu), a.iters)
         print(f"linear M={a.M} N={a.N} K={a.K}: {us:.1f} us, {2.0 * a.M * a.N * a.K / us / 1e6:.1f} TFLOP/s")
+    elif a.op == "linear_act":
+        kind, out = torch.float8_e4m3fn if a.e4m3 else torch.bfloat16, torch.float32 if a.f32out else torch.bfloat16
+        x, w = torch.randn(a.M, a.K, device=dev).to(kind), torch.randn(a.N, a.K, device=dev).to(kind)
+        y, bias = torch.empty(a.M, a.N, device=dev, dtype=out), torch.randn(a.N, device=dev)
+        res = torch.randn(a.M, a.N, device=dev).to(out) if a.residual else None
+        scales = dict(x_scale=torch.full((a.M,), 0.01, device=dev), w_scale=torch.full((a.N,), 0.01, device=dev)) if a.e4m3 else {}
+        us = _time(lambda: api.grace_linear_act(x, w, y, bias=bias, act=a.act, residual=res, **scales), a.iters)
+        print(f"linear_act M={a.M} N={a.N} K={a.K} {kind}: {us:.1f} us, {2.0 * a.M * a.N * a.K / us / 1e6:.1f} TFLOP/s")
+    elif a.op == "rms_norm":
+        R = a.B * a.M
+        x = torch.randn(R, a.K, device=dev).to(torch.float32 if a.f32out else torch.bfloat16)
+        delta, gamma = (bf(R, a.K) if a.residual else None), torch.ones(a.K, device=dev)
+        out = torch.empty(R, a.K, device=dev, dtype=torch.float8_e4m3fn if a.e4m3 else torch.bfloat16)
+        scale, xo = (torch.empty(R, device=dev) if a.e4m3 else None), (torch.empty_like(x) if a.residual else None)
+        us = _time(lambda: api.grace_rms_norm(x, gamma, out, delta=delta, x_out=xo, scale=scale), a.iters)
+        by = R * a.K * (x.element_size() * (2 if a.residual else 1) + (2 if a.residual else 0) + out.element_size())
+        print(f"rms_norm R={R} D={a.K}: {us:.1f} us, {by / us / 1e3:.0f} GB/s")
+    elif a.op == "sample":
+        R = a.B * a.M
+        logits = torch.randn(R, a.V, device=dev) * 3
+        if a.bf16stream:
+            logits = logits.to(torch.bfloat16)
+        bits = None
+        if a.density < 1.0:
+            bits = torch.zeros(R, (a.V + 63) // 64, dtype=torch.int64, device=dev)
+            for bit in range(64):
+                bits |= (torch.rand(bits.shape, device=dev) < a.density).to(torch.int64) << bit
+        full = lambda v, t=torch.float32: torch.full((a.B,), v, dtype=t, device=dev)
+        T, k, p, q = full(a.temperature), full(a.topk, torch.int32), full(a.topp), full(a.minp)
+        u, sc = torch.rand(R, a.draws, device=dev), torch.empty(R * a.draws, device=dev)
+        tk = torch.empty(R * a.draws, dtype=torch.int32, device=dev)
+        us = _time(lambda: api.grace_sample(logits, u, sc, tk, a.B, a.M, allow_bits=bits, temperature=T, top_k=k, top_p=p, min_p=q), a.iters)
+        by = (a.density if bits is not None else 1.0) * logits.numel() * logits.element_size() + (0 if bits is None else bits.numel() * 8)
+        print(f"sample R={R} V={a.V}: {us:.1f} us, {by / us / 1e3:.0f} GB/s of allowed logits and bits")
     elif a.op == "row_stats":
         R = a.B * a.M
         xs = [bf(R, a.K) for _ in range(3)]                # rotated: 3 x R x K x 2 bytes, larger than L2 at R = 65536
