@@ -756,7 +756,9 @@ static grace_status_t linear_act_impl(const void* x, int64_t ldx, const float* x
       (residual == y && ldr != ldy) ||
       ((reinterpret_cast<uintptr_t>(x_scale) | reinterpret_cast<uintptr_t>(w_scale) | reinterpret_cast<uintptr_t>(bias)) & 3))
     return GRACE_INVALID_ARG;
-  if (K % kPer16) return GRACE_UNSUPPORTED_SHAPE;
+  // (tiles' ends are int; without columns for the persistent kernel, row tiles are gridDim.y)
+  constexpr int kMost = 0x7fffffff - 255;
+  if (K % kPer16 || M > kMost || N > kMost || K > kMost || (!linear_pair_possible(M, N, false) && M > 65535 * kGemmBM)) return GRACE_UNSUPPORTED_SHAPE;
   ActParams p;
   p.x_scale = x_scale; p.w_scale = w_scale; p.bias = bias; p.residual = residual; p.y = y;
   p.ldr = ldr; p.ldy = ldy; p.M = M; p.N = N; p.KB = (K + kBK - 1) / kBK; p.act = act;

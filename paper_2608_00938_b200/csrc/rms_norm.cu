@@ -243,7 +243,7 @@ extern "C" grace_status_t grace_rms_norm(const float* x_f32, const uint16_t* x_b
       (reinterpret_cast<uintptr_t>(gamma) & 3) || (reinterpret_cast<uintptr_t>(y_bf16) & 1) || (reinterpret_cast<uintptr_t>(y_scale) & 3) ||
       (x_out == x && ldx_out != ldx))
     return GRACE_INVALID_ARG;
-  if (D > kRmsMostD) return GRACE_UNSUPPORTED_SHAPE;
+  if (D > kRmsMostD || R > 0x7fffffff - 3) return GRACE_UNSUPPORTED_SHAPE;              // (four rows a CTA, counted in int)
   RmsParams p;
   p.x = x; p.delta = delta; p.x_out = x_out; p.gamma = gamma;
   p.y = y_bf16 != nullptr ? (void*)y_bf16 : (void*)y_e4m3;

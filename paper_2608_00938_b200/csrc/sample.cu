@@ -17,9 +17,10 @@ extern "C" grace_status_t grace_sample(const float* logits_f32, const uint16_t* 
   const uintptr_t words = reinterpret_cast<uintptr_t>(logits_f32) | reinterpret_cast<uintptr_t>(row_score) | reinterpret_cast<uintptr_t>(row_lse) |
                           reinterpret_cast<uintptr_t>(temperature) | reinterpret_cast<uintptr_t>(top_k) | reinterpret_cast<uintptr_t>(top_p) |
                           reinterpret_cast<uintptr_t>(min_p) | reinterpret_cast<uintptr_t>(u) | reinterpret_cast<uintptr_t>(out_score) |
-                          reinterpret_cast<uintptr_t>(out_logq) | reinterpret_cast<uintptr_t>(out_parent) | reinterpret_cast<uintptr_t>(out_token);
+                          reinterpret_cast<uintptr_t>(out_logq) | reinterpret_cast<uintptr_t>(out_parent) | reinterpret_cast<uintptr_t>(out_token) |
+                          reinterpret_cast<uintptr_t>(d_status);
   if ((words & 3) || (reinterpret_cast<uintptr_t>(logits_bf16) & 1) || (reinterpret_cast<uintptr_t>(allow_bits) & 7)) return GRACE_INVALID_ARG;
-  if (V > kSampleMostV || (int64_t)B * M > 0x7fffffffll) return GRACE_UNSUPPORTED_SHAPE;
+  if (V > kSampleMostV || draws > kSampleMostDraws || (int64_t)B * M > 0x7fffffffll) return GRACE_UNSUPPORTED_SHAPE;
   SampleParams p = {};
   const bool bf16 = logits_bf16 != nullptr;
   p.logits = bf16 ? (const void*)logits_bf16 : (const void*)logits_f32;

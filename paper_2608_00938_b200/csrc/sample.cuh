@@ -42,7 +42,7 @@ struct SampleParams {
 constexpr int kSampleBuckets = 256;
 // Steps of the histogram: 256 over 22 powers of two of weight; the last one holds all that is lighter.
 constexpr float kSampleSteps = 256.f / 22.f;
-constexpr int kSampleMostV = 65536;
+constexpr int kSampleMostV = 65536, kSampleMostDraws = 1 << 30;
 
 __device__ __forceinline__ float sample_ex2(float x) {
   float y;

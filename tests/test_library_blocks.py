@@ -95,3 +95,21 @@ def test_quantized_rows_are_the_oracles(api):
             api.grace_quantize_rows_e4m3(w2)
     with pytest.raises(ValueError):
         api.grace_quantize_rows_e4m3(w[0])
+
+
+INT_MAX = 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("sizes", [
+    dict(M=65535 * 128 + 1, N=255, ldy=255),                 # more row tiles than a grid takes, too few columns for the persistent kernel
+    dict(M=65535 * 128 + 1), dict(M=INT_MAX), dict(N=INT_MAX - 200, ldy=INT_MAX), dict(M=1, K=INT_MAX - 15, ldx=INT_MAX - 15, ldw=INT_MAX - 15),
+])
+def test_linear_act_refuses_sizes_whose_tiles_it_cannot_count(api, e4m3, sizes):
+    assert _linear(api, e4m3, **sizes) == SHAPE
+
+
+def test_norm_and_sample_refuse_sizes_that_they_cannot_count(api):
+    assert _norm(api, R=INT_MAX) == SHAPE and _norm(api, R=INT_MAX - 2) == SHAPE
+    assert _sample(api, draws=2 ** 30 + 1) == SHAPE and _sample(api, draws=INT_MAX) == SHAPE
+    assert _sample(api, st=P + 2) == INVALID
