@@ -64,9 +64,10 @@ __device__ __forceinline__ float act_gelu_one(float v) {
   return fmaf(-a, act_ex2(q), max_nan(v, 0.f));
 }
 __device__ __forceinline__ void act_gelu_bf16(float& v0, float& v1) { v0 = act_gelu_one(v0); v1 = act_gelu_one(v1); }
+// (1 + erf is 0 from -5.7 on; v at -64 there, so that -inf times 0 is no NaN)
 __device__ __forceinline__ void act_gelu_f32(float& v0, float& v1) {
-  v0 = 0.5f * v0 * (1.f + erff(v0 * 0.70710678118654752f));
-  v1 = 0.5f * v1 * (1.f + erff(v1 * 0.70710678118654752f));
+  v0 = 0.5f * max_nan(v0, -64.f) * (1.f + erff(v0 * 0.70710678118654752f));
+  v1 = 0.5f * max_nan(v1, -64.f) * (1.f + erff(v1 * 0.70710678118654752f));
 }
 // The activation of a whole array: one branch for all of it (one per element is an indirect branch each: 65536 x 2048 x 512
 // took 463 us so, without any activation).
@@ -109,6 +110,11 @@ struct ActCfg {
   static_assert(kSlice % 16 == 0 && kTotal <= 227 * 1024, "");
 };
 constexpr int kActThreads = 192;                           // four row warps, TMA producer, MMA issuer
+// The tensor cores' accumulator drops what it cannot hold at every step, towards zero: 6.2e-8 of the result per k-block of four steps
+// (root mean square, normal operands), 5e-6 over K = 8192 in this kernel's longest chains, where an fp32 product on the cores
+// is off by 5e-7.  So fp32 results of more k-blocks than this are added up segment by segment outside, rounded to nearest: 6.8e-7 at
+// 500 x 1000 x 8192 in 16.2 us (segments of 16: 9.97e-7, 15.6 us; of 8: 4.7e-7, 16.5 us).
+constexpr int kActSegment = 12;
 
 template <bool F8, bool F32, int BN, int STAGES, int SPLIT>
 __global__ void __launch_bounds__(kActThreads, 2)
@@ -123,8 +129,10 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
   float* col_s = reinterpret_cast<float*>(tiles + STAGES * S::kStageBytes + S::kXBytes); // [kSlice] scales, [kSlice] biases
   uint64_t* full = reinterpret_cast<uint64_t*>(tiles + STAGES * S::kStageBytes + S::kXBytes + S::kColBytes);
   uint64_t* empty = full + STAGES;
-  uint64_t* accum_bar = empty + STAGES;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(accum_bar + 1);
+  uint64_t* accum_bar = empty + STAGES;                    // [2]: a segment's products are done
+  uint64_t* drained = accum_bar + 2;                       // the row warps have taken a segment behind the first
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
+  constexpr int kTmemCols = F32 ? 2 * BN : (BN < 32 ? 32 : BN);   // fp32: the sum, and a segment
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -135,14 +143,14 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
   if (SPLIT > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // "this CTA has started"
   if (threadIdx.x == 0) {
     for (int s = 0; s < STAGES; ++s) { tc::mbar_init(full + s, 1); tc::mbar_init(empty + s, 1); }
-    tc::mbar_init(accum_bar, 1);
+    tc::mbar_init(accum_bar, 1); tc::mbar_init(accum_bar + 1, 1); tc::mbar_init(drained, 4);
     *abort_flag = 0;
     tc::fence_mbar_init();
   }
   if (warp == 4) {
     if (lane == 0) { tc::tma_prefetch_desc(&map_x); tc::tma_prefetch_desc(&map_w); }
     __syncwarp();
-    tc::tmem_alloc(tmem_slot, BN < 32 ? 32 : BN);
+    tc::tmem_alloc(tmem_slot, kTmemCols);
   }
   tc::tc_fence_before();
   __syncthreads();
@@ -171,19 +179,30 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
   } else if (warp == 5) {
     if (lane == 0) {
       constexpr uint32_t idesc = act_idesc<F8>(kGemmBM, BN);
-      for (int kb = 0; kb < KB; ++kb) {
-        const int s = kb % STAGES;
-        if (!tc::mbar_wait(full + s, (kb / STAGES) & 1, abort_flag)) break;
-        tc::tc_fence_after();
-        const uint32_t a_addr = tc::smem_addr(tiles + s * S::kStageBytes);
-        const uint64_t a_desc = tc::smem_desc_sw128(a_addr, 16, 1024);
-        const uint64_t b_desc = tc::smem_desc_sw128(a_addr + S::kABytes, 16, 1024);
+      bool issued = true;
+      for (int kb0 = 0, seg = 0; issued && kb0 < KB; kb0 += kActSegment, ++seg) {
+        const int kb1 = F32 ? min(kb0 + kActSegment, KB) : KB;
+        if (F32 && seg >= 2) {
+          if (!tc::mbar_wait(drained, seg & 1, abort_flag)) break;
+          tc::tc_fence_after();
+        }
+        const uint32_t d_tmem = tmem_base + (F32 && seg > 0 ? (uint32_t)BN : 0u);
+        for (int kb = kb0; kb < kb1; ++kb) {
+          const int s = kb % STAGES;
+          issued = tc::mbar_wait(full + s, (kb / STAGES) & 1, abort_flag);
+          if (!issued) break;
+          tc::tc_fence_after();
+          const uint32_t a_addr = tc::smem_addr(tiles + s * S::kStageBytes);
+          const uint64_t a_desc = tc::smem_desc_sw128(a_addr, 16, 1024);
+          const uint64_t b_desc = tc::smem_desc_sw128(a_addr + S::kABytes, 16, 1024);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-          act_mma<F8, false>(tmem_base, a_desc + (uint64_t)(2 * k), b_desc + (uint64_t)(2 * k), idesc, (kb | k) ? 1u : 0u);
-        tc::mma_commit(empty + s);
+          for (int k = 0; k < 4; ++k)
+            act_mma<F8, false>(d_tmem, a_desc + (uint64_t)(2 * k), b_desc + (uint64_t)(2 * k), idesc, (kb > kb0 || k) ? 1u : 0u);
+          tc::mma_commit(empty + s);
+        }
+        tc::mma_commit(accum_bar + (seg & 1));
+        if (!F32) break;
       }
-      tc::mma_commit(accum_bar);
     }
     __syncwarp();
   } else {
@@ -195,6 +214,35 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
     ok = tc::mbar_wait(accum_bar, 0, abort_flag);
     ok = __all_sync(kFullMask, ok);
     tc::tc_fence_after();
+    if constexpr (F32) {
+      const uint32_t sum = tmem_base + ((uint32_t)(warp * 32) << 16);
+      for (int seg = 1; ok && seg * kActSegment < KB; ++seg) {
+        ok = tc::mbar_wait(accum_bar + (seg & 1), (seg >> 1) & 1, abort_flag);
+        ok = __all_sync(kFullMask, ok);
+        tc::tc_fence_after();
+        if (!ok) break;
+#pragma unroll 1
+        for (int c = 0; c < BN; c += 32) {
+          uint32_t a[2][16], b[2][16];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            tc::tmem_ld16(sum + c + 16 * h, a[h]);
+            tc::tmem_ld16(sum + BN + c + 16 * h, b[h]);
+          }
+          tc::tmem_ld_wait();
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) a[h][j] = __float_as_uint(__uint_as_float(a[h][j]) + __uint_as_float(b[h][j]));
+            tc::tmem_st16(sum + c + 16 * h, a[h]);
+          }
+        }
+        tc::tmem_st_wait();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(drained);
+      }
+    }
     tc::named_bar_sync(1, 128);                            // the column vectors of all four warps
   }
   const uint32_t t_acc = tmem_base + ((uint32_t)((warp & 3) * 32) << 16);
@@ -318,7 +366,7 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
   }
   tc::tc_fence_before();
   __syncthreads();
-  if (warp == 4) tc::tmem_dealloc(tmem_base, BN < 32 ? 32 : BN);
+  if (warp == 4) tc::tmem_dealloc(tmem_base, kTmemCols);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -330,9 +378,10 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 // registers one step ahead, from there into the 2 KB, and a thread adds its row's where the results will lie.  No warp waits
 // for another.  WIDE: rows of y and of the residual start on 16 bytes; otherwise the warp moves single elements between the
 // 2 KB and memory.
-// LONG (fp32 results of more than 16 k-blocks): the tensor cores' accumulator drops what it cannot hold at every step, towards
-// zero, and over 512 steps that adds up to 5e-6 of the result.  So an accumulator takes 16 k-blocks, and the epilogue's warps
-// add them up in registers, rounded to nearest, while the other accumulator fills.
+// LONG (fp32 results of more than kAPSegment k-blocks): an accumulator takes a segment, and the epilogue's warps add them up in
+// registers while the other accumulator fills.  Segments of 16 k-blocks leave 1.0e-6 of the result; of 12, 7.3e-7 for 7 to 25 % more
+// time (7003 x 2036 x 8184 with SiLU and residual 285 -> 305 us, 20000 x 1024 x 1024 43 -> 53: the accumulators change hands
+// before they are drained); with a first one of 32 while the tile in front is finished, 281 us and 2.1e-6 at K = 2048.
 // (Eight warps in two groups that share a buffer and its barriers: 84 us for 65536 x 2048 x 512 in e4m3, without activation.)
 // ---------------------------------------------------------------------------------------------
 constexpr int kAPStages = 5;
@@ -343,9 +392,7 @@ constexpr int kAPTurn = 32 * kAPRow;
 constexpr int kAPCols = 2 * kAPWarpCols * 4;               // scales and biases of the warp's columns
 constexpr int kAPSmem = kAPStages * kAPStageBytes + kAPWarps * (kAPTurn + kAPCols) + 256;
 constexpr int kAPThreads = 64 + 32 * kAPWarps;
-// k-blocks that LONG leaves to one accumulator; a tile's first, during which the tile in front is finished, has twice as many
-constexpr int kAPSegment = 16;
-__device__ __forceinline__ int act_segment_end(int kb) { return kb + (kb == 0 ? 2 * kAPSegment : kAPSegment); }
+constexpr int kAPSegment = 16;                              // LONG: k-blocks of an accumulator
 static_assert(kAPSmem >= tc::kTmemAllSmem && kAPSmem <= 227 * 1024, "");
 
 // v = acc * xs * scale + bias of N columns, whose scales and biases (kAPWarpCols behind the scales) lie in shared memory.
@@ -434,7 +481,7 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         bool ok = true;
         for (int kb0 = 0, kb1; ok && kb0 < p.KB; kb0 = kb1, ++local) {
           const int ab = local & 1;
-          kb1 = LONG ? min(act_segment_end(kb0), p.KB) : p.KB;
+          kb1 = LONG ? min(kb0 + kAPSegment, p.KB) : p.KB;
           ok = tc::mbar_wait_cluster(acc_empty + ab, ((local >> 1) & 1) ^ 1, abort_flag);
           if (!ok) break;
           tc::tc_fence_after();
@@ -528,14 +575,14 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
       if constexpr (LONG) {
         // All segments but the last into registers; with the last they go back into its accumulator, and on as one.  (64 of a
         // thread's 96 registers: nothing of the finish is fetched ahead, and the accumulator is read by eights.  What does not fit
-        // goes to the L2 and back, the shared memory having left no L1: 13 us a tile.)
+        // goes to the L2 and back, the shared memory having left no L1.)
         float sum[kAPWarpCols / 8][8];
         bool ok = true;
-        for (int kb0 = 0; kb0 < p.KB; kb0 = act_segment_end(kb0)) {
+        for (int kb0 = 0; kb0 < p.KB; kb0 += kAPSegment) {
           ok = wait_full();
           if (!ok) break;
           const uint32_t t = t_acc();
-          const bool last = act_segment_end(kb0) >= p.KB;
+          const bool last = kb0 + kAPSegment >= p.KB;
 #pragma unroll
           for (int c = 0; c < kAPWarpCols / 8; ++c) {
             uint32_t r[8];

@@ -261,6 +261,24 @@ def test_linear_of_small_integers_is_exact(api, M, N, K, e4m3):
     assert torch.equal(y, (x @ w.T + b).clamp_min(0) + r)
 
 
+@pytest.mark.parametrize("M,N", [(1, 40), (16, 64), (130, 500), (200, 2000), (700, 1000), (1000, 8000), (1100, 300), (2500, 512)])
+@pytest.mark.parametrize("e4m3,K", [(False, 16384), (True, 32768), (False, 1096), (False, 2120), (True, 6160)])
+def test_long_sums_do_not_drift(api, M, N, e4m3, K):
+    """Products of positive numbers, whose running sums grow evenly (a step adds 16 or 32 products of mean 1).  An accumulator that cuts
+    off what it cannot hold loses at most a last place, 2^-23 of the sum so far, at each of a segment's steps; there are 128 at the
+    most and the sums so far are half the segment's on average: 64 x 2^-23 of it, and an eighth more for the evenness.  The sums of
+    16 segments at the most, of four CTAs and the epilogue are rounded to nearest: 24 x 2^-24.  (1024 steps without segments: 512
+    x 2^-23 by the same count.)"""
+    g = gen(M + N)
+    kind = E4M3 if e4m3 else BF
+    x = (torch.rand(M, K, device=DEV, generator=g) + 0.5).to(kind)
+    w = (torch.rand(N, K, device=DEV, generator=g) + 0.5).to(kind)
+    y = torch.empty(M, N, device=DEV)
+    api.grace_linear_act(x, w, y)
+    want = x.double() @ w.double().T
+    assert float(((y.double() - want).abs() / want).max()) <= 84 * 2.0 ** -23
+
+
 def test_linear_of_large_values(api):
     """Activations far out: no NaN from an overflowing exponential, zero or the value itself."""
     v = torch.tensor([-1e30, -3e4, -300.0, -90.0, -41.0, -20.0, -16.0, -6.0, 0.0, 6.0, 16.0, 41.0, 90.0, 300.0, 3e4, 1e30], device=DEV).to(BF)
@@ -278,6 +296,21 @@ def test_linear_of_large_values(api):
                 got = f64(y[:16, 7])
                 assert np.isfinite(got).all()
                 assert (np.abs(got - ref) <= 2.0 ** -7.9 * np.abs(ref) + 2e-5).all(), (act, got, ref)
+
+
+def test_linear_columns_of_infinite_biases(api):
+    """A bias of -inf takes a column out: the smooth activations' limits are 0 (silu's and tanh's forms stop at 64 2^-60 = 2^-54)."""
+    for M in (40, 1200):
+        x, w, _, _ = operands(gen(4), M, 300, 160, False)
+        b = torch.zeros(300, device=DEV)
+        b[7::10], b[3::50] = -float("inf"), float("inf")
+        for act in ("relu", "gelu", "gelu_tanh", "silu"):
+            for kind in (BF, F32):
+                y = torch.empty(M, 300, device=DEV, dtype=kind)
+                api.grace_linear_act(x, w, y, bias=b, act=act)
+                assert (y[:, 7::10].abs() <= 2.0 ** -53).all() and (y[:, 3::50] == float("inf")).all(), (act, kind)
+                rest = torch.isfinite(b)
+                assert torch.isfinite(y[:, rest]).all()
 
 
 def test_linear_keeps_a_bad_row_to_itself(api):
