@@ -5,13 +5,15 @@
 //   A draw takes the first kept token, in ascending order, at which the running sum of kept weights exceeds u times the whole.
 //
 // A warp has a row of up to 2048 tokens, a CTA a longer one (or one of few).  A pass or two over the row leave a list of the
-// elements that can be kept: those of at least min-p's bound, of the histogram steps down to the one that holds the top_k-th, or
+// elements that can be kept: those of at least min-p's bound, of the histogram steps down to the one that holds the top_k-th or top-p's cut, or
 // heavy enough for top-p (a set whose weights are all at most (1 - p) S / n weighs at most (1 - p) S, so nothing of it is
 // needed to reach p S).  With a constraint the list is the allowed tokens.  Everything else happens on the list, in shared
 // memory.  The loops are rolled: unrolled over a row in registers, the same steps waited for instructions six cycles of
 // fourteen.
 // No sort: the cut is found through a histogram of 256 equal steps of (max - x) / T, in counts (top-k) or in fixed-point
 // weights (top-p), whose one step that holds the cut is then resolved value by value.
+// Measured (65536 x 2048 fp32, one draw; a read at the rate of a copy takes 82 us): no limit 304 us, T = 0 142, min-p 0.02 221, top-k 50
+// 326, top-k 200 with top-p 0.95 and min-p 0.02 475; a twentieth allowed, top-p 0.9 180.  Bound by instructions and the latency of dependent ones.
 // The answer is that of the definition in 64 bits, at the cost of 32: weights and sums are fp32, every comparison of a sum with
 // a border has a margin above the sums' worst error, and a row for which one falls inside the margin is done again with
 // e^ and sums in fp64.
@@ -872,6 +874,12 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   if (l.min_p > 0.f) l.least = min_p_bound(m, l.min_p, sc.t);
   float bound = by_count && l.top_p < 1.f ? -INFINITY : l.least;
   Sum<NW> whole_row = 0;
+  // a step's far edge, further by what rounding can make of it
+  auto edge = [&](int step) { return m - ((float)(step + 1) * 1.0001f) / (sc.c * kSampleSteps) - fabsf(m) * 0x1p-20f; };
+  // top-p: the weights' histogram leaves what is kept and a step or two; the bound on light weights alone, several times that.
+  // (65536 x 2048, top-p 0.95 at T = 1.5: 1515 us by the latter, 1090 so; 0.9 of bf16 logits 641, 560; 1024 x 16384, top-p
+  // 0.9: 142, 131.  The longest rows, of which few draw and whose threads meet in the same steps: 64 x 65472, top-p 0.95: 49, 52.)
+  constexpr bool kMassHist = NW <= 8;
   if (by_count) {
     clear_hist(tm, sh);
     tm.sync();
@@ -887,9 +895,7 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
     find_bucket(tm, sh, [&](uint32_t) { return (uint32_t)l.top_k; });
     l.step = sh.bucket;
     l.step_above = (int)sh.above;
-    // the step's far edge, further by what rounding can make of it
-    if (l.step >= 0 && l.step < kSampleBuckets - 1)
-      bound = fmaxf(bound, m - ((float)(l.step + 1) * 1.0001f) / (sc.c * kSampleSteps) - fabsf(m) * 0x1p-20f);
+    if (l.step >= 0 && l.step < kSampleBuckets - 1) bound = fmaxf(bound, edge(l.step));
   } else if (by_mass) {
     Sum<NW> s0 = 0, s1 = 0, s2 = 0, s3 = 0;
     const double c64 = NW == 1 ? 0. : 1.4426950408889634 / (double)sc.t;
@@ -897,12 +903,36 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
       if constexpr (NW == 1) return sample_ex2((x - m) * sc.c);
       else return sample_ex2_fine(((double)x - (double)m) * c64);
     };
-#pragma unroll (NW == 1 ? 4 : 2)
+    // the weights' histogram as well, in fixed point as narrow()'s
+    const float scale = __uint_as_float((uint32_t)(126 + __clz(p.V - 1)) << 23);
+    if (kMassHist) {
+      clear_hist(tm, sh);
+      tm.sync();
+    }
+    auto add = [&](float x, Sum<NW>& sum) {
+      const Sum<NW> w = weight(x);
+      sum += w;
+      if (kMassHist) {
+        const uint32_t share = __float2uint_rn((float)w * scale);
+        if (share != 0u) atomicAdd(&sh.hist[sample_bucket(m, x, sc.c)], share);
+      }
+    };
+#pragma unroll 2
     for (int i = 0; i < iters; ++i) {
       const float4 t = quad(first + 32 * i);
-      s0 += weight(t.x); s1 += weight(t.y); s2 += weight(t.z); s3 += weight(t.w);
+      add(t.x, s0); add(t.y, s1); add(t.z, s2); add(t.w, s3);
     }
     whole_row = tm.sum((s0 + s1) + (s2 + s3));
+    if (kMassHist) {
+      // The step at which the running sum has reached top_p of the whole for sure: a share is off by half a unit at most and
+      // 2^-18.4 of itself (22 times the roundings of x - m, log2(e) / T and their product).
+      tm.sync();
+      find_bucket(tm, sh, [&](uint32_t all) {
+        const float want = (float)all * fmaxf(l.top_p, 0.f) * (1.f + 0x1p-16f) + (float)p.V;
+        return min((uint32_t)fminf(want, 4294967040.f), all);
+      });
+      if (sh.bucket >= 0 && sh.bucket < kSampleBuckets - 1) bound = fmaxf(bound, edge(sh.bucket));
+    }
     const float light = (1.f - fmaxf(l.top_p, 0.f)) * (float)whole_row / (float)n * 0.999f;
     bound = fmaxf(bound, m + log2f(light) / sc.c - 1e-4f / sc.c - fabsf(m) * 0x1p-20f);
   }
@@ -1131,6 +1161,8 @@ template <bool BF16>
 static grace_status_t run_sample(const SampleParams& p, cudaStream_t s) {
   // Warps of a row: one per 2048 tokens at least, more while the GPU is not filled by the rows (a pass over a row is then as
   // long as its threads' part).
+  // Rows in a list's shared memory: half the tokens' room.  (With 3/8 of it 20 warps instead of 18 are on an SM, 8 % less time for short
+  // lists, but top-k 1000 of 2048 goes from 517 to 670 us, its row being read again.)
   const bool lists = p.allow != nullptr;
   if (p.V > 16384) return lists ? launch_sample<32, BF16, true>(p, s) : launch_sample<32, BF16, false>(p, s);
   if (p.V > 8192 || (p.V > 1024 && p.R <= kSms)) return lists ? launch_sample<8, BF16, true>(p, s) : launch_sample<8, BF16, false>(p, s);
