@@ -925,11 +925,12 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
     whole_row = tm.sum((s0 + s1) + (s2 + s3));
     if (kMassHist) {
       // The step at which the running sum has reached top_p of the whole for sure: a share is off by half a unit at most and
-      // 2^-18.4 of itself (22 times the roundings of x - m, log2(e) / T and their product).
+      // 2^-18.4 of itself (22 times the roundings of x - m, log2(e) / T and their product).  None where that is beyond the whole:
+      // what has less than half a unit is not in it.
       tm.sync();
       find_bucket(tm, sh, [&](uint32_t all) {
         const float want = (float)all * fmaxf(l.top_p, 0.f) * (1.f + 0x1p-16f) + (float)p.V;
-        return min((uint32_t)fminf(want, 4294967040.f), all);
+        return want < (float)all ? (uint32_t)want : 0xffffffffu;
       });
       if (sh.bucket >= 0 && sh.bucket < kSampleBuckets - 1) bound = fmaxf(bound, edge(sh.bucket));
     }

@@ -113,6 +113,22 @@ def test_masked_rows_match_the_definition(api, B, M, V, density):
     check(api, logits.to(BF), numbers(V + 1, R, 1), B, M, allow=allow, p=[0.95] * B)
 
 
+@pytest.mark.parametrize("V", [300, 1001, 2048, 5000, 16384])
+def test_top_p_that_reaches_into_the_lightest(api, V):
+    """One heavy token and many whose weights are next to nothing one by one, and together what top_p still wants."""
+    rng = np.random.default_rng(V)
+    powers = np.array([8.0, 12.0, 17.0, 19.0, 20.5, 20.99, 21.01, 21.9, 22.1, 23.0])
+    x = -np.log(2.0) * powers[:, None] * np.ones((1, V)) + rng.normal(size=(10, V)) * 1e-4
+    x[np.arange(10), rng.integers(0, V, 10)] = 0.0
+    logits = torch.tensor(x, dtype=F32, device=DEV)
+    u = torch.tensor([[0.3, 0.9993, 0.9999, 0.9999995]] * 10, dtype=F32)
+    light = np.exp(x).sum(1) - 1.0
+    for share in (0.1, 0.5, 0.9):                            # of the light ones' weight
+        p = [(1.0 + share * w) / (1.0 + w) for w in light]
+        check(api, logits, u, 10, 1, p=p)
+        check(api, logits, u, 10, 1, p=p, allow=rng.random((10, V)) < 0.95)
+
+
 @pytest.mark.parametrize("V", [50, 700, 2048, 6000, 30000])
 def test_ties(api, V):
     """Equal logits: the whole row, two values, few values, signed zeros; the lower token goes first."""
