@@ -537,8 +537,8 @@ grace_status_t grace_log_softmax(float* logits, int R, int V, void* stream);
  * x_out (x's type) are both given or both NULL (s = x, nothing kept); x_out may be x, with its row stride.  Otherwise
  * outputs overlap nothing.  Row r of a tensor starts at r * its row stride (elements, >= D).  The norm is that of the
  * stored stream: one call with delta gives the bits of an addition followed by a call without.
- * Statistics in fp32.  A NaN stays in its row, whose y_scale is then NaN.  1 <= D <= 16384, R <= 2^31 - 4, any alignment of the
- * elements' own; rows that all start on 16 bytes (y_e4m3: 8) with D % 8 == 0 take the wide form. */
+ * Statistics in fp32.  A NaN stays in its row, whose y_scale is then NaN.  1 <= D <= 16384, R <= 2^31 - 4, any alignment
+ * of the elements' own; rows that all start on 16 bytes (y_e4m3: 8) with D % 8 == 0 take the wide form. */
 grace_status_t grace_rms_norm(const float* x_f32, const uint16_t* x_bf16, int64_t ldx, const uint16_t* delta,
                               int64_t ld_delta, void* x_out, int64_t ldx_out, const float* gamma,
                               uint16_t* y_bf16, uint8_t* y_e4m3, int64_t ldy, float* y_scale,
@@ -559,9 +559,9 @@ typedef enum {
 /* y = act(x @ w^T + bias) + residual: grace_linear with a bias, the activations above and a residual of y's type behind
  * them.  x bf16 [M][K] (row stride ldx), w bf16 [N][K] (ldw), bias fp32 [N] or NULL; exactly one of y_bf16 / y_f32 ([M][N],
  * row stride ldy); residual: same type as y, [M][N], row stride ldr, or NULL; it may be y itself (ldr = ldy), otherwise y
- * overlaps nothing.  fp32 accumulation (fp32 results: about 1e-6 off, root mean square), one rounding of the result.  x and w 16-byte aligned with row strides that are
- * multiples of 8 elements, K a multiple of 8; M, N, and the alignment of y, residual and bias (their elements' own) are free
- * (M <= 128 * 65535 with N < 256). */
+ * overlaps nothing.  fp32 accumulation (fp32 results: about 1e-6 off, root mean square), one rounding of the result.
+ * x and w 16-byte aligned with row strides that are multiples of 8 elements, K a multiple of 8; M, N, and the alignment of
+ * y, residual and bias (their elements' own) are free (M <= 128 * 65535 with N < 256; all sizes <= 2^31 - 256). */
 grace_status_t grace_linear_act(const uint16_t* x, int64_t ldx, const uint16_t* w, int64_t ldw, const float* bias, int act,
                                 const void* residual, int64_t ldr, uint16_t* y_bf16, float* y_f32, int64_t ldy,
                                 int M, int N, int K, void* stream);
