@@ -798,67 +798,6 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
   }
 }
 
-// A step's far edge, further by what rounding can make of it.
-__device__ __forceinline__ float step_edge(float m, int step, float c) { return m - ((float)(step + 1) * 1.0001f) / (c * kSampleSteps) - fabsf(m) * 0x1p-20f; }
-// The sum of a row's weights, and a bound below which top-p keeps nothing.  (Out of line: its loop beside that of top-k's counts cost rows
-// that need the latter alone 5 %: 506 us instead of 473 for
-// 65536 x 2048 with every limit.)
-template <int NW>
-struct MassBound {
-  Sum<NW> whole;
-  float bound;
-};
-template <int NW, bool BF16, bool SHARED>
-static __device__ __noinline__ MassBound<NW> mass_bound(const RowGlobal<BF16> row, const float4* const shared, const Team<NW> tm, SampleShared<NW>* const sh, const float m,
-                                                        const Scale sc, const float top_p, const int n, const int iters, const int first) {
-  // top-p: the weights' histogram leaves what is kept and a step or two; the bound on light weights alone, several times that.
-  // (65536 x 2048, top-p 0.95 at T = 1.5: 1515 us by the latter, 1090 so; 0.9 of bf16 logits 641, 560; 1024 x 16384, top-p
-  // 0.9: 142, 131.  The longest rows, of which few draw and whose threads meet in the same steps: 64 x 65472, top-p 0.95: 49, 52.)
-  constexpr bool kMassHist = NW <= 8;
-  const int quads = (row.n + 3) >> 2;
-  const float p = fmaxf(top_p, 0.f);
-  Sum<NW> s0 = 0, s1 = 0, s2 = 0, s3 = 0;
-  const double c64 = NW == 1 ? 0. : 1.4426950408889634 / (double)sc.t;
-  // in fixed point as narrow()'s
-  const float scale = __uint_as_float((uint32_t)(126 + __clz(row.n - 1)) << 23);
-  if (kMassHist) {
-    clear_hist(tm, *sh);
-    tm.sync();
-  }
-  auto add = [&](float x, Sum<NW>& sum) {
-    Sum<NW> w;
-    if constexpr (NW == 1) w = sample_ex2((x - m) * sc.c);
-    else w = sample_ex2_fine(((double)x - (double)m) * c64);
-    sum += w;
-    if (kMassHist) {
-      const uint32_t share = __float2uint_rn((float)w * scale);
-      if (share != 0u) atomicAdd(&sh->hist[sample_bucket(m, x, sc.c)], share);
-    }
-  };
-#pragma unroll 2
-  for (int i = 0; i < iters; ++i) {
-    const int q = first + 32 * i;
-    const float4 t = SHARED ? shared[q] : (q < quads ? row.quad(q) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY));
-    add(t.x, s0); add(t.y, s1); add(t.z, s2); add(t.w, s3);
-  }
-  MassBound<NW> by;
-  by.whole = tm.sum((s0 + s1) + (s2 + s3));
-  const float light = (1.f - p) * (float)by.whole / (float)n * 0.999f;
-  by.bound = m + log2f(light) / sc.c - 1e-4f / sc.c - fabsf(m) * 0x1p-20f;
-  if (kMassHist) {
-    // The step at which the running sum has reached top_p of the whole for sure: a share is off by half a unit at most and
-    // 2^-18.4 of itself (22 times the roundings of x - m, log2(e) / T and their product).  None where that is beyond the whole:
-    // what has less than half a unit is not in it.
-    tm.sync();
-    find_bucket(tm, *sh, [&](uint32_t all) {
-      const float want = (float)all * p * (1.f + 0x1p-16f) + (float)row.n;
-      return want < (float)all ? (uint32_t)want : 0xffffffffu;
-    });
-    if (sh->bucket >= 0 && sh->bucket < kSampleBuckets - 1) by.bound = fmaxf(by.bound, step_edge(m, sh->bucket, sc.c));
-  }
-  return by;
-}
-
 // A row without a list yet: dense, or with more allowed tokens than a list takes.  SHARED (one warp): the row lies in the list's
 // place and is narrowed there; otherwise every pass reads it.
 template <int NW, bool BF16, bool SHARED>
@@ -935,6 +874,12 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   if (l.min_p > 0.f) l.least = min_p_bound(m, l.min_p, sc.t);
   float bound = by_count && l.top_p < 1.f ? -INFINITY : l.least;
   Sum<NW> whole_row = 0;
+  // a step's far edge, further by what rounding can make of it
+  auto edge = [&](int step) { return m - ((float)(step + 1) * 1.0001f) / (sc.c * kSampleSteps) - fabsf(m) * 0x1p-20f; };
+  // top-p: the weights' histogram leaves what is kept and a step or two; the bound on light weights alone, several times that.
+  // (65536 x 2048, top-p 0.95 at T = 1.5: 1515 us by the latter, 1090 so; 0.9 of bf16 logits 641, 560; 1024 x 16384, top-p
+  // 0.9: 142, 131.  The longest rows, of which few draw and whose threads meet in the same steps: 64 x 65472, top-p 0.95: 49, 52.)
+  constexpr bool kMassHist = NW <= 8;
   if (by_count) {
     clear_hist(tm, sh);
     tm.sync();
@@ -950,11 +895,47 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
     find_bucket(tm, sh, [&](uint32_t) { return (uint32_t)l.top_k; });
     l.step = sh.bucket;
     l.step_above = (int)sh.above;
-    if (l.step >= 0 && l.step < kSampleBuckets - 1) bound = fmaxf(bound, step_edge(m, l.step, sc.c));
+    if (l.step >= 0 && l.step < kSampleBuckets - 1) bound = fmaxf(bound, edge(l.step));
   } else if (by_mass) {
-    const MassBound<NW> by = mass_bound<NW, BF16, SHARED>(row, shared, tm, &sh, m, sc, l.top_p, n, iters, first);
-    whole_row = by.whole;
-    bound = fmaxf(bound, by.bound);
+    Sum<NW> s0 = 0, s1 = 0, s2 = 0, s3 = 0;
+    const double c64 = NW == 1 ? 0. : 1.4426950408889634 / (double)sc.t;
+    auto weight = [&](float x) -> Sum<NW> {
+      if constexpr (NW == 1) return sample_ex2((x - m) * sc.c);
+      else return sample_ex2_fine(((double)x - (double)m) * c64);
+    };
+    // the weights' histogram as well, in fixed point as narrow()'s
+    const float scale = __uint_as_float((uint32_t)(126 + __clz(p.V - 1)) << 23);
+    if (kMassHist) {
+      clear_hist(tm, sh);
+      tm.sync();
+    }
+    auto add = [&](float x, Sum<NW>& sum) {
+      const Sum<NW> w = weight(x);
+      sum += w;
+      if (kMassHist) {
+        const uint32_t share = __float2uint_rn((float)w * scale);
+        if (share != 0u) atomicAdd(&sh.hist[sample_bucket(m, x, sc.c)], share);
+      }
+    };
+#pragma unroll 2
+    for (int i = 0; i < iters; ++i) {
+      const float4 t = quad(first + 32 * i);
+      add(t.x, s0); add(t.y, s1); add(t.z, s2); add(t.w, s3);
+    }
+    whole_row = tm.sum((s0 + s1) + (s2 + s3));
+    if (kMassHist) {
+      // The step at which the running sum has reached top_p of the whole for sure: a share is off by half a unit at most and
+      // 2^-18.4 of itself (22 times the roundings of x - m, log2(e) / T and their product).  None where that is beyond the whole:
+      // what has less than half a unit is not in it.
+      tm.sync();
+      find_bucket(tm, sh, [&](uint32_t all) {
+        const float want = (float)all * fmaxf(l.top_p, 0.f) * (1.f + 0x1p-16f) + (float)p.V;
+        return want < (float)all ? (uint32_t)want : 0xffffffffu;
+      });
+      if (sh.bucket >= 0 && sh.bucket < kSampleBuckets - 1) bound = fmaxf(bound, edge(sh.bucket));
+    }
+    const float light = (1.f - fmaxf(l.top_p, 0.f)) * (float)whole_row / (float)n * 0.999f;
+    bound = fmaxf(bound, m + log2f(light) / sc.c - 1e-4f / sc.c - fabsf(m) * 0x1p-20f);
   }
   if (by_count || by_mass || l.min_p > 0.f) {
     bound = fmaxf(fminf(bound, m), -3.402823466e38f);      // (-inf is in no list)
