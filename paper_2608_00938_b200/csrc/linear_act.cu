@@ -380,9 +380,10 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 // 2 KB and memory.
 // LONG (fp32 results of more than kAPSegment k-blocks): an accumulator takes a segment, and the epilogue's warps add them up in
 // registers while the other accumulator fills.  Segments of 16 k-blocks leave 1.0e-6 of the result; of 12, 7.3e-7 for 7 to 25 % more
-// time (7003 x 2036 x 8184 with SiLU and residual 285 -> 305 us, 20000 x 1024 x 1024 43 -> 53: the accumulators change hands
+// time (7003 x 2036 x 8184 with SiLU and residual 283 -> 305 us, 20000 x 1024 x 1024 43 -> 53: the accumulators change hands
 // before they are drained); with a first one of 32 while the tile in front is finished, 281 us and 2.1e-6 at K = 2048.
-// (Eight warps in two groups that share a buffer and its barriers: 84 us for 65536 x 2048 x 512 in e4m3, without activation.)
+// Measured, e4m3 to bf16: 65536 x 2048 x 512 89 us (eight warps in two groups that share a buffer and its barriers: 84), with GELU
+// 130, bound by the epilogue's instructions; 65536 x 512 x 2048 61 us, 2.26 PFLOP/s, 68 with a residual.
 // ---------------------------------------------------------------------------------------------
 constexpr int kAPStages = 5;
 constexpr int kAPStageBytes = 2 * 128 * 128;
