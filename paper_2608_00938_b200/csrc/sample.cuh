@@ -53,11 +53,11 @@ __device__ __forceinline__ float sample_ex2(float x) {
 }
 // What weights are and are added up in before 64 bits decide.  A warp's rows are many and short: fp32, and one in some dozens
 // is done again.  In a CTA's rows, of up to 65536 tokens, a border is next to some sum nearly always, and the one row that is done
-// again holds up the call (64 x 65472, top-p 0.95: 70 us, 28 without): fp64, with an e^ that is good to 2^-32.
+// again holds up the call (64 x 65472, top-p 0.95: 70 us, 28 without): fp64, with an e^ that is good to 2.8e-10.
 template <int NW>
 using Sum = std::conditional_t<NW == 1, float, double>;
-// 2^y for y <= 0 to 2^-32 of itself: 2^floor times the Taylor polynomial of degree 8 of 2^f, |f| <= 1/2
-// ((ln 2 / 2)^9 / 9! = 2e-10); 2^-1000 and less come out as about 2^-1000.
+// 2^y for y <= 0 to 2.8e-10 of itself: 2^floor times the Taylor polynomial of degree 8 of 2^f, |f| <= 1/2
+// ((ln 2 / 2)^9 / 9! = 2e-10, of 2^-1/2 at the least); 2^-1000 and less come out as about 2^-1000.
 __device__ __forceinline__ double sample_ex2_fine(double y) {
   y = fmax(y, -1000.);
   const double magic = 6755399441055744.;                  // 3 x 2^51: the sum's last bits are the nearest integer
@@ -282,7 +282,6 @@ struct Sampler {
   float temperature;
   using W = Sum<NW>;
   double c64;                    // log2(e) / T, for fp64 sums
-  W margin;                      // of sums, relative to the whole
   int group;                     // elements of a table entry
   // top-p counts elements that the list leaves out: their weight with the list's (0: the row is all there is), and where they are
   W whole_row;
@@ -296,11 +295,40 @@ struct Sampler {
     else return sample_ex2_fine(((double)x - (double)m) * c64);
   }
   __device__ __forceinline__ double weight64(float x) const { return sample_weight64(x, m, temperature); }
+  // What a comparison of two sums can be off by at the most, the weights' sum being `whole`.  In fp32 (a warp's rows: at most 2048 tokens, group <= 16),
+  // in units of 2^-24 of the whole: `steps` (below) and the weights' own errors, which count once for both sums: the exponent's, 3.5 of z = (max - x) / T
+  // (the difference, log2(e) / T, the product), whose mean over the weights is at most ln 2048 - ln whole (a distribution's entropy is at most ln n).
+  // The steps: 4 of ex2, and one for each addition that an addend passes at most.
+  //   cut    top_p of the whole: 15 + 2 + 5 (sample_dense) or 7 + 7 + 5 (narrow), and the product: 23.  The sum in front: 7 + 7 + 5, and the
+  //          list's to it: 20.  The difference, the ties' weight and its quotient: 4.  In all 51.
+  //   draw   u of the whole: group - 1 + 3 + 5 (tabulate), and the product: group + 8.  The running sum: group + 7, three entries of the table, and an
+  //          element: by a scan of five (pick_together) group + 11 in all, or after up to group others (pick) 2 group + 10.  Two for the
+  //          comparisons.  In all 25 + 2 group, 24 + 3 group.
+  // In fp64: 2.8e-10 of a weight's (sample_ex2_fine), the rest below 2^-44.
+  __device__ __forceinline__ W off_by(float steps, W whole) const {
+    if constexpr (NW == 1) return (steps + 2.43f * (11.f - __log2f(whole))) * 0x1p-24f * whole;
+    else return 1e-9 * whole;
+  }
   __device__ __forceinline__ int bucket_of(float x) const { return sample_bucket(m, x, c); }
   template <class F>
   __device__ __forceinline__ void for_each(F f) const {
 #pragma unroll 2
     for (int i = tm.tid; i < row.n; i += NT) f(row.at(i), i);
+  }
+  // The same where sums are formed (SUMS; else for_each): f(x, place) for eight elements of a thread at a time, then done(): a sum by eights and of the eights
+  // passes 8 + n / (8 NT) additions instead of n / NT, which is what its error goes by.
+  template <bool SUMS, class F, class Done>
+  __device__ __forceinline__ void for_each_by_eights(F f, Done done) const {
+    if (!SUMS) {
+      for_each(f);
+      return;
+    }
+#pragma unroll 1
+    for (int i0 = tm.tid; i0 < row.n; i0 += 8 * NT) {
+#pragma unroll 2
+      for (int i = i0; i < min(i0 + 8 * NT, row.n); i += NT) f(row.at(i), i);
+      done();
+    }
   }
   __device__ __forceinline__ void note(float t, int r, int same) const {
     shared->found_t = t; shared->found_r = r; shared->found_all = r == same; shared->found = 1;
@@ -339,20 +367,24 @@ struct Sampler {
     // the step's values; fixed point may have missed the step by a little: then its neighbour's
     for (int tries = 0; ; ++tries) {
       whole = above = W(0);
-      W inside = W(0);
-      for_each([&](float x, int place) {
+      W inside = W(0), whole_8 = W(0), above_8 = W(0);
+      for_each_by_eights<MASS>([&](float x, int place) {
         if (!cut.keeps(x, place)) return;
         const int at = bucket_of(x);
         if (MASS) {
           const W w = weight(x);
-          whole += w;
-          above += at < b ? w : W(0);
+          whole_8 += w;
+          above_8 += at < b ? w : W(0);
           if (NW > 1) inside += at == b ? w : W(0);
         }
         if (at == b) {
           const int i = atomicAdd(&shared->n_list, 1);
           if (i < kList) shared->list[i] = x;
         }
+      }, [&]() {
+        whole += whole_8;
+        above += above_8;
+        whole_8 = above_8 = W(0);
       });
       if (MASS) {
         whole = whole_row > W(0) ? whole_row : tm.sum(whole);
@@ -382,14 +414,19 @@ struct Sampler {
       const float x = shared->list[i];
       int same = 0;
       if (MASS) {
-        W front = above;
-        for (int j = 0; j < len; ++j) {
-          const float y = shared->list[j];
-          if (y > x) front += weight(y);
-          same += y == x;
+        W front = W(0);
+        for (int j0 = 0; j0 < len; j0 += 8) {
+          W front_8 = W(0);
+          for (int j = j0; j < min(j0 + 8, len); ++j) {
+            const float y = shared->list[j];
+            if (y > x) front_8 += weight(y);
+            same += y == x;
+          }
+          front += front_8;
         }
+        front += above;
         same *= copies;
-        const W w = weight(x), gap = (W)p * whole - front, slack = margin * whole;
+        const W w = weight(x), gap = (W)p * whole - front, slack = off_by(51.f, whole);
         if (gap > slack && gap + slack < w * (W)same) {
           const W q = gap / w, r = ceil(q);
           if (same == 1 || ((r - q) * w > slack && (q - (r - W(1))) * w > slack)) note(x, min(same, max(1, (int)r)), same);
@@ -479,13 +516,16 @@ struct Sampler {
       const int at = max(0, shared->bucket);
       key_hi -= (uint32_t)at << shift;
       key_lo = max(key_lo, key_hi - ((1u << shift) - 1u));
-      W more = W(0);
+      W more = W(0), more_8 = W(0);
       int inside = 0, over = 0;
-      for_each([&](float x, int place) {
+      for_each_by_eights<MASS>([&](float x, int place) {
         if (!cut.keeps(x, place)) return;
         const uint32_t key = ordered_key(x);
-        if (key > key_hi) { over += 1; if (MASS) more += weight(x); }
+        if (key > key_hi) { over += 1; if (MASS) more_8 += weight(x); }
         else if (key >= key_lo) inside += 1;
+      }, [&]() {
+        more += more_8;
+        more_8 = W(0);
       });
       n = tm.sum(inside);
       n_above = tm.sum(over);
@@ -759,17 +799,15 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
                                                const RowLimits& l, const Scale& sc, Sum<NW> whole_row, const LeftOut<BF16>& rest, bool infinite) {
   constexpr int NT = NW * 32;
   using S = Sampler<NW, Row, LeftOut<BF16>>;
-  // Sums' worst error, relative to the whole.  A weight's: its exponent's, 3.5 x 2^-24 of z = (max - x) / T (the difference, c, the
-  // product), whose mean over the weights is at most ln V (a distribution's entropy is); 2^-22 of ex2.  A sum's: 2^-24 for each of
-  // the 30 additions that an addend passes at most: 3.3e-6 for V = 2048.  In fp64: 2^-32 of a weight's, the rest below 2^-45.
-  const Sum<NW> margin = NW == 1 ? Sum<NW>(3.4e-6) : Sum<NW>(1e-9);
-  const int group = (row.n + 4 * NT - 1) / (4 * NT);
-  const S s{row, tm, &sh, m, sc.c, sc.t, NW == 1 ? 0. : 1.4426950408889634 / (double)sc.t, margin, Row::kQuads ? (group + 3) & ~3 : group, whole_row, rest};
+  const int quarter = (row.n + 4 * NT - 1) / (4 * NT), group = Row::kQuads ? (quarter + 3) & ~3 : quarter;
+  // few draws: a warp together for one after the other; many: each thread its own
+  const bool together = p.draws <= 8;
+  const S s{row, tm, &sh, m, sc.c, sc.t, NW == 1 ? 0. : 1.4426950408889634 / (double)sc.t, group, whole_row, rest};
   Cut cut = {-INFINITY, -1};
   if (l.top_k > 0 && l.top_k < row.n) cut = s.template narrow<false>(cut, l.top_k, 0.f, l.step, l.step_above);
   if (l.top_p < 1.f) cut = s.template narrow<true>(cut, 0, fmaxf(l.top_p, 0.f), -1, 0);
   if (l.least > cut.t) cut = Cut{l.least, 0x7fffffff};
-  const Sum<NW> whole = s.template tabulate<false>(cut);
+  const Sum<NW> whole = s.template tabulate<false>(cut), slack = s.off_by((float)(together ? 25 + 2 * group : 24 + 3 * group), whole);
   const float log_whole = logf((float)whole);
   auto store = [&](int d, int place) {
     place = max(place, 0);
@@ -777,8 +815,6 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
     store_draw(p, l, r, d, row.token(place), infinite ? INFINITY : x, (x - m) / sc.t - log_whole);
   };
   bool have64 = false;
-  // few draws: a warp together for one after the other; many: each thread its own
-  const bool together = p.draws <= 8;
   for (int d0 = 0; d0 < p.draws; d0 += together ? 1 : NT) {
     const int d = d0 + (together ? 0 : tm.tid);
     const bool in = d < p.draws && (!together || tm.tid < 32);
@@ -787,7 +823,7 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
     bool sure = false;
     int place = -1;
     if (!have64 && in) {
-      place = together ? s.pick_together(cut, whole, u, s.margin * whole, sure) : s.template pick<false>(cut, whole, u, s.margin * whole, sure);
+      place = together ? s.pick_together(cut, whole, u, slack, sure) : s.template pick<false>(cut, whole, u, slack, sure);
     }
     const int doubt = tm.reduce(in && !sure ? 1 : 0, [](int a, int e) { return a | e; });
     if (doubt) {
