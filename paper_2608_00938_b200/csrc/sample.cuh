@@ -554,8 +554,23 @@ struct Sampler {
   // by bisection over all values.  Sets shared->found_*.
   static __device__ __noinline__ void narrow64(const Sampler s, const Cut cut, const float p, const int len, const int copies) { s.narrow64_(cut, p, len, copies); }
   __device__ __forceinline__ void narrow64_(const Cut cut, const float p, const int len, const int copies) const {
-    float top = -INFINITY;
-    for (int j = 0; j < len; ++j) top = fmaxf(top, shared->list[j]);
+    // the list in descending order: its sums then do not depend on which thread came first
+    constexpr int kPer = (kList + NT - 1) / NT;
+    float own[kPer];
+    int at[kPer];
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+      const int i = tm.tid + e * NT;
+      own[e] = i < len ? shared->list[i] : 0.f;
+      at[e] = 0;
+      for (int j = 0; j < len; ++j) at[e] += shared->list[j] > own[e] || (shared->list[j] == own[e] && j < i);
+    }
+    tm.sync();
+#pragma unroll
+    for (int e = 0; e < kPer; ++e)
+      if (tm.tid + e * NT < len) shared->list[at[e]] = own[e];
+    tm.sync();
+    const float top = len > 0 ? shared->list[0] : -INFINITY;
     double whole = 0., above = 0.;
     for_each([&](float x, int place) {
       if (!cut.keeps(x, place)) return;
@@ -570,17 +585,20 @@ struct Sampler {
     auto settle = [&](float x, double front, int same) {
       note(x, min(same, max(1, (int)fmin(ceil((goal - front) / weight64(x)), 2147483647.))), same);
     };
+    // (a value's sum ends where the next one's begins, so one value is found at the most)
     for (int i = tm.tid; i < len; i += NT) {
       const float x = shared->list[i];
+      const double w = weight64(x);
       double front = above;
-      int same = 0;
-      for (int j = 0; j < len; ++j) {
-        const float y = shared->list[j];
-        if (y > x) front += weight64(y);
-        same += y == x;
+      int j = 0, same = 0;
+      for (; shared->list[j] > x; ++j) front += weight64(shared->list[j]);
+      double end = front;
+      for (; j < len && shared->list[j] == x; ++j, ++same) end += w;
+      if (copies > 1) {
+        same = copies;
+        end = front + w * same;
       }
-      same *= copies;
-      if ((front < goal || (front == 0. && goal <= 0.)) && front + weight64(x) * same >= goal) settle(x, front, same);
+      if ((front < goal || (front == 0. && goal <= 0.)) && end >= goal) settle(x, front, same);
     }
     tm.sync();
     if (shared->found != 0) return;

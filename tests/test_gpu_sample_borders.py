@@ -68,3 +68,25 @@ def test_numbers_beside_a_border(api, R, V, draws):
         for d in range(draws):
             u[r, d] = beside(run[rng.integers(0, V - 1)], rng.integers(-1, 2))
     check(api, x, u, 1, R)
+
+
+def test_rows_decided_in_64_bits_repeat(api):
+    """Rows that 64 bits decide, on two streams: no result depends on the order in which threads add to a list."""
+    R, V = 1500, 2048
+    rng = np.random.default_rng(3)
+    x = logits_for(5, R, V, std=0.5)
+    xd = x.double().cpu().numpy()
+    run = np.cumsum(np.exp(-np.sort(-xd, 1)), 1)
+    run /= run[:, -1:]
+    p = torch.tensor([beside(run[r, rng.integers(0, V - 2)], 0) for r in range(R)], device=DEV)
+    u = torch.full((R, 1), 1 - 2.0 ** -24, device=DEV)
+    outs, streams = [], [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for i in range(6):
+        with torch.cuda.stream(streams[i % 2]):
+            sc, lq, tk = torch.empty(R, device=DEV), torch.empty(R, device=DEV), torch.empty(R, device=DEV, dtype=torch.int32)
+            api.grace_sample(x, u, sc, tk, R, 1, top_p=p, out_logq=lq)
+            outs.append((sc, lq, tk))
+    torch.cuda.synchronize()
+    for o in outs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(o, outs[0]))
