@@ -387,7 +387,12 @@ struct Sampler {
         whole_8 = above_8 = W(0);
       });
       if (MASS) {
-        whole = whole_row > W(0) ? whole_row : tm.sum(whole);
+        whole = tm.sum(whole);
+        if (whole_row > W(0)) {
+          // A list that min-p has cut shorter than top-p would: all of it stays, and no border is near.
+          if ((W)p * whole_row - whole > off_by(51.f, whole_row)) return cut;
+          whole = whole_row;
+        }
         above = tm.sum(above);
       }
       tm.sync();
