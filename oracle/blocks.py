@@ -45,6 +45,10 @@ def row_scales(n):
     return np.maximum(np.abs(n).max(axis=1), 2.0 ** -100) / 448.0
 
 
+def _logistic(z):
+    return np.where(z >= 0, 1.0, np.exp(-np.abs(z))) / (1.0 + np.exp(-np.abs(z)))
+
+
 def activation(v, act):
     v = np.asarray(v, dtype=np.float64)
     if act == "relu":
@@ -52,7 +56,8 @@ def activation(v, act):
     if act == "gelu":
         return v * 0.5 * np.vectorize(math.erfc, otypes=[np.float64])(-v / math.sqrt(2.0))
     if act == "gelu_tanh":
-        return 0.5 * v * (1.0 + np.tanh(math.sqrt(2.0 / math.pi) * (v + 0.044715 * v ** 3)))
+        # (1 + tanh z) / 2 = 1 / (1 + e^-2z), which keeps its digits where tanh z is next to -1
+        return v * _logistic(2.0 * math.sqrt(2.0 / math.pi) * (v + 0.044715 * v ** 3))
     if act == "silu":
-        return v * np.where(v >= 0, 1.0 / (1.0 + np.exp(-np.abs(v))), np.exp(-np.abs(v)) / (1.0 + np.exp(-np.abs(v))))
+        return v * _logistic(v)
     return v
