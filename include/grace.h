@@ -560,6 +560,8 @@ typedef enum {
  * them.  x bf16 [M][K] (row stride ldx), w bf16 [N][K] (ldw), bias fp32 [N] or NULL; exactly one of y_bf16 / y_f32 ([M][N],
  * row stride ldy); residual: same type as y, [M][N], row stride ldr, or NULL; it may be y itself (ldr = ldy), otherwise y
  * overlaps nothing.  fp32 accumulation (fp32 results: about 1e-6 off, root mean square), one rounding of the result.
+ * The smooth activations are good to a few fp32 roundings of their exponents (GELU's Phi(-|v|) to bf16: 2^-16 of itself, to fp32:
+ * 2^-20 up to |v| = 2, 2^-18 up to 5); what is nearer to 0 than 2^-54 comes out within that of 0.
  * x and w 16-byte aligned with row strides that are multiples of 8 elements, K a multiple of 8; M, N, and the alignment of
  * y, residual and bias (their elements' own) are free (M <= 128 * 65535 with N < 256; all sizes <= 2^31 - 256). */
 grace_status_t grace_linear_act(const uint16_t* x, int64_t ldx, const uint16_t* w, int64_t ldw, const float* bias, int act,

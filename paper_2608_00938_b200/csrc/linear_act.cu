@@ -51,23 +51,47 @@ __device__ __forceinline__ void act_gelu_tanh(float& v0, float& v1) {
   // (1 + tanh z) / 2 = 1 / (1 + e^-2z), 2z = sqrt(8 / pi) (v + 0.044715 v^3), times log2(e)
   act_over_pair(v0, v1, v0 * fmaf(v0 * v0, -0.10294324f, -2.3022082f), v1 * fmaf(v1 * v1, -0.10294324f, -2.3022082f));
 }
-// v Phi(v) = max(v, 0) - a Phi(-a), a = |v|, and Phi(-a) = 2^P(a) with P of degree 5: log2 Phi(-a) is smooth and nearly
-// quadratic.  P is a minimax fit of it on [0, 5] (weighted least squares, reweighted by the error): Phi(-a) is within 7.5e-5 of
-// itself, 1 / 26 of half a bf16 step, and P goes on falling behind.  For bf16 results; fp32 ones take erff.
-__device__ __forceinline__ float act_gelu_one(float v) {
-  const float a = fminf(fabsf(v), 16.f);
-  float q = fmaf(a, -3.292835899628699e-4f, 5.912758409976959e-3f);
-  q = fmaf(a, q, -4.852477088570595e-2f);
-  q = fmaf(a, q, -4.6373286843299866e-1f);
-  q = fmaf(a, q, -1.149355173110962f);
-  q = fmaf(a, q, -1.000108003616333f);
+// v Phi(v) = max(v, 0) - a Phi(-a), a = |v|, and Phi(-a) = 2^P(a): log2 Phi(-a) is smooth and nearly quadratic.  P is a fit of it for
+// the smallest greatest error (least squares over Chebyshev nodes, reweighted by the error), coefficients rounded to fp32 from the highest on
+// and the others fitted again.  Phi(-a) is then off, by fit and roundings (P falls to -63) and the exponential, by less than
+//   bf16 results, degree 8 up to a = 9       2^-16 of itself: 1 / 128 of half a bf16 step
+//   fp32 results, degree 12 up to a = 8.6    2^-20.3 up to 2, 2^-18.5 up to 5, 2^-15.7 up to 8.6
+// From there on a stays, and what is left is above -2^-54.  (1 + erff has no digits left at -5.7; erfcf has, but took 342 us for 65536 x 2048 x 512
+// e4m3 to fp32.)
+__device__ __forceinline__ float act_gelu_one_f32(float v) {
+  const float a = fminf(fabsf(v), 8.6f);
+  float q = fmaf(a, -7.3320009785771134e-11f, 4.0688297175961452e-09f);
+  q = fmaf(a, q, -1.0023314445106735e-07f);
+  q = fmaf(a, q, 1.4398045777852531e-06f);
+  q = fmaf(a, q, -1.3235676306067035e-05f);
+  q = fmaf(a, q, 7.87459357525222e-05f);
+  q = fmaf(a, q, -0.00026501136017031968f);
+  q = fmaf(a, q, -6.315719656413421e-05f);
+  q = fmaf(a, q, 0.0070560760796070099f);
+  q = fmaf(a, q, -0.052534673362970352f);
+  q = fmaf(a, q, -0.45918348431587219f);
+  q = fmaf(a, q, -1.1511095762252808f);
+  q = fmaf(a, q, -0.99999994039535522f);
   return fmaf(-a, act_ex2(q), max_nan(v, 0.f));
 }
-__device__ __forceinline__ void act_gelu_bf16(float& v0, float& v1) { v0 = act_gelu_one(v0); v1 = act_gelu_one(v1); }
-// (1 + erf is 0 from -5.7 on; v at -64 there, so that -inf times 0 is no NaN)
-__device__ __forceinline__ void act_gelu_f32(float& v0, float& v1) {
-  v0 = 0.5f * max_nan(v0, -64.f) * (1.f + erff(v0 * 0.70710678118654752f));
-  v1 = 0.5f * max_nan(v1, -64.f) * (1.f + erff(v1 * 0.70710678118654752f));
+__device__ __forceinline__ void act_gelu_f32(float& v0, float& v1) { v0 = act_gelu_one_f32(v0); v1 = act_gelu_one_f32(v1); }
+// (packed: 65536 x 2048 x 512 e4m3 152 -> 127 us; rows of y that do not start on 16 bytes, 20000 x 1001 x 1024, 41 -> 43)
+__device__ __forceinline__ void act_gelu_bf16(float& v0, float& v1) {
+  const float a0 = fminf(fabsf(v0), 9.f), a1 = fminf(fabsf(v1), 9.f);
+  const f32x2_t a = f2_pack(a0, a1);
+  auto both = [](float c) { return f2_pack(c, c); };
+  f32x2_t q = f2_fma(a, both(7.4632509949879022e-08f), both(-3.6557726161845494e-06f));
+  q = f2_fma(a, q, both(7.9437530075665563e-05f));
+  q = f2_fma(a, q, both(-1.0200483957305551e-03f));
+  q = f2_fma(a, q, both(8.7508680298924446e-03f));
+  q = f2_fma(a, q, both(-5.4304659366607666e-02f));
+  q = f2_fma(a, q, both(-4.5824155211448669e-01f));
+  q = f2_fma(a, q, both(-1.1512949466705322f));
+  q = f2_fma(a, q, both(-0.9999966025352478f));
+  float q0, q1;
+  f2_unpack(q, q0, q1);
+  v0 = fmaf(-a0, act_ex2(q0), max_nan(v0, 0.f));
+  v1 = fmaf(-a1, act_ex2(q1), max_nan(v1, 0.f));
 }
 // The activation of a whole array: one branch for all of it (one per element is an indirect branch each: 65536 x 2048 x 512
 // took 463 us so, without any activation).
