@@ -168,17 +168,25 @@ rms_norm_kernel(const RmsParams p) {
   }
 
   if (E4M3) {
-    // (a row of zeros gets zeros and the least scale; so does what 448 / most would overflow for)
+    // (a row of zeros gets zeros and the least scale, whose reciprocal is an fp32 number)
     most = max_nan(reduce(most, 1), 0x1p-100f);
-    const float inv = 448.f / most;
-    if (tid == 0) p.scale[r] = most / 448.f;
+    const float scale = most / 448.f;
+    if (tid == 0) p.scale[r] = scale;
+    // n / scale by the reciprocal and the quotient's remainder (Markstein's correction): the fp32 quotient, so that values next to one of
+    // e4m3's borders go as the definition has them.  65536 x 512: 39.3 us, by the reciprocal alone 38.9, by divisions 42.3.  (An infinite
+    // scale has no remainder.)
+    const float inv = 1.f / scale, take = isinf(scale) ? 0.f : scale;
+    auto over = [&](float n) {
+      const float q = n * inv;
+      return fmaf(fmaf(-take, q, take == 0.f ? 0.f : n), inv, q);
+    };
     uint8_t* yrow = reinterpret_cast<uint8_t*>(p.y) + (int64_t)r * p.ldy;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       uint32_t q[2] = {0, 0};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
-        q[e >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v[i][2 * e] * inv, v[i][2 * e + 1] * inv), __NV_SATFINITE, __NV_E4M3) << (16 * (e & 1));
+        q[e >> 1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(over(v[i][2 * e]), over(v[i][2 * e + 1])), __NV_SATFINITE, __NV_E4M3) << (16 * (e & 1));
       if (VEC) {
         const int c = i * NT + tid;
         if (c < n8) reinterpret_cast<uint2*>(yrow)[c] = make_uint2(q[0], q[1]);

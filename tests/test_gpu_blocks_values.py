@@ -87,3 +87,39 @@ def test_logistic_forms(api, M, act, kind):
     bound = off + (2.0 ** -8 if kind == BF else 2.0 ** -24) * (np.abs(ref) + off)
     i = (err / bound).argmax()
     assert (err <= bound).all(), (x[i], err[i], ref[i])
+
+
+@pytest.mark.parametrize("D", [16384, 8191, 4096, 1024, 1023])
+def test_norm_divides_by_the_scale(api, D):
+    """y = n / y_scale, rounded once more, for n exactly gamma (rows of ones): values next to e4m3's borders."""
+    rng = np.random.default_rng(D)
+    for stream in (F32, BF):
+        for _ in range(6):
+            most = np.float32(rng.uniform(0.5, 40))
+            scale = np.float32(most / np.float32(448))
+            middles = (OB.E4M3[1:] + OB.E4M3[:-1]) / 2
+            near = np.float32(rng.choice(middles, D) * float(scale))
+            near = np.clip((near.view(np.int32) + rng.integers(-4, 5, D).astype(np.int32)).view(np.float32), None, most) * rng.choice(np.float32([-1, 1]), D)
+            near[rng.integers(D)] = most
+            gamma = torch.tensor(near, dtype=F32, device=DEV)
+            x = torch.ones(3, D, device=DEV, dtype=stream)
+            out, s = torch.empty(3, D, device=DEV, dtype=E4M3), torch.empty(3, device=DEV)
+            api.grace_rms_norm(x, gamma, out, 0.0, scale=s)
+            assert (s.cpu().numpy() == scale).all()
+            want = OB.to_e4m3((near / scale).astype(np.float32))
+            got = out.view(torch.uint8).cpu().numpy()
+            assert (got == want).all(), int((got != want).sum())
+
+
+def test_norm_whose_scale_is_infinite(api):
+    """A gain that overflows takes its own element, not the row's others."""
+    x = torch.full((2, 512), 1e-3, device=DEV)
+    x[0, 7] = 20.0
+    gamma = torch.ones(512, device=DEV)
+    gamma[7] = 3e38
+    out, s = torch.empty(2, 512, device=DEV, dtype=E4M3), torch.empty(2, device=DEV)
+    api.grace_rms_norm(x, gamma, out, scale=s)
+    assert s[0].item() == float("inf") and torch.isfinite(s[1])
+    q = out.float()
+    assert torch.isnan(q[0, 7]) and (q[0, :7] == 0).all() and (q[0, 8:] == 0).all()
+    assert q[1, 7] == 448
