@@ -221,7 +221,7 @@ def _rows(t, where: str, name: str, dtype, device: int, shape=None):
     rows, width = t.shape
     if one != 1 and width != 1:
         _refuse(where, f"{name} has no contiguous rows")
-    return t.data_ptr(), (ld if rows > 1 or ld > width else width)
+    return t.data_ptr(), (ld if rows > 1 else width)
 
 
 def version() -> int:

@@ -123,3 +123,14 @@ def test_norm_whose_scale_is_infinite(api):
     q = out.float()
     assert torch.isnan(q[0, 7]) and (q[0, :7] == 0).all() and (q[0, 8:] == 0).all()
     assert q[1, 7] == 448
+
+
+def test_a_single_row_of_any_stride(api):
+    """One row out of a wider matrix: its stride says nothing."""
+    g = torch.Generator(device=DEV)
+    g.manual_seed(1)
+    wide = torch.randn(1, 520, device=DEV, generator=g).to(BF).as_strided((1, 512), (513, 1))
+    w = torch.randn(64, 512, device=DEV, generator=g).to(BF)
+    y = torch.empty(1, 64, device=DEV)
+    api.grace_linear_act(wide, w, y)
+    assert (y.double() - wide.double() @ w.double().T).abs().max() <= 2.0 ** -19 * (wide.double().abs() @ w.double().abs().T).max()
