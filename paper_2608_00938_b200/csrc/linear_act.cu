@@ -282,6 +282,7 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 #pragma unroll
         for (int c = 0; c < kSlice; c += 16) {
           uint32_t acc[16];
+          __syncwarp();                                    // (rows behind the last one store nothing: together again for the load)
           tc::tmem_ld16(t_acc + (uint32_t)(dst * kSlice + c), acc);
           tc::tmem_ld_wait();
           if (m < p.M) {
@@ -309,6 +310,7 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 #pragma unroll 1
     for (int c = 0; c < kSlice; c += 16) {
       uint32_t acc[16];
+      __syncwarp();                                        // (rows behind the last one left the turn in front early)
       tc::tmem_ld16(t_acc + (uint32_t)(rank * kSlice + c), acc);
       const int n = slice0 + c;
       const bool in = m < p.M && n < p.N, whole = n + 16 <= p.N;
@@ -642,6 +644,7 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
         if (F8) scale[32 * i + lane] = ws_next[i];
         scale[kAPWarpCols + 32 * i + lane] = bias_next[i];
       }
+      __syncwarp();                                         // every lane reads all of them
       if (!LONG) fetch(tile_m * 256 + (int)rank * 128 + q * 32, tile_n * p.bn + col);
       // the finished columns c0 .. of the tile: scales, bias, activation, residual, and out
       auto finish = [&](const int c0, const uint32_t (&r)[kCols]) {
@@ -712,6 +715,7 @@ act_pair_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant
 #pragma unroll 1
       for (int c0 = 0; c0 < kAPWarpCols; c0 += kCols) {
         uint32_t r[kCols];
+        __syncwarp();                                       // (lanes part in the step in front's stores)
         if constexpr (F32) tc::tmem_ld16(t + c0, r); else tc::tmem_ld32(t + c0, r);
         tc::tmem_ld_wait();
         if (c0 + kCols == kAPWarpCols) give_back();         // this part of the accumulator has been read
