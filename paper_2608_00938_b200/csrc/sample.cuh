@@ -1019,6 +1019,7 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
         uint32_t at = (uint32_t)(kept + (__popc(b0 & below) + __popc(b1 & below)) + (__popc(b2 & below) + __popc(b3 & below)));
         kept += all;
         if (kept > p.tokens_cap) break;
+        __syncwarp();                                      // these 128 have been read by all lanes: the list may come over them
         const int token = 4 * (32 * i + lane);
         take(t.x, at, token); take(t.y, at, token + 1); take(t.z, at, token + 2); take(t.w, at, token + 3);
       }
