@@ -593,7 +593,7 @@ grace_status_t grace_linear_act_e4m3(const uint8_t* x, int64_t ldx, const float*
  * A NaN among a row's allowed logits sets GRACE_DEV_NAN and leaves the row without candidates.  Logits of +inf weigh
  * 1 each and all others nothing.
  * The tokens are those of this definition in 64-bit arithmetic.  Nothing depends on the order of the GPU's threads.
- * V <= 65536, draws <= 2^30, B*M < 2^31; T counts as 1e30 at most. */
+ * V <= 65536, draws <= 2^30, B*M < 2^31; a positive T counts as 1e-36 at least and 1e30 at most. */
 grace_status_t grace_sample(const float* logits_f32, const uint16_t* logits_bf16, int64_t ld, const uint64_t* allow_bits,
                             const float* row_score, const float* row_lse, const float* temperature,
                             const int32_t* top_k, const float* top_p, const float* min_p, const float* u,

@@ -796,8 +796,8 @@ __device__ __forceinline__ RowLimits row_limits(const SampleParams& p, int64_t r
   return l;
 }
 struct Scale {                   // of the weights
-  float t, c;                    // T, log2(e) / T
-  __device__ __forceinline__ explicit Scale(float temperature) : t(fminf(temperature, 1e30f)), c(fminf(1.44269504f / t, 1e38f)) {}
+  float t, c;                    // T, held where log2(e) / T and the histogram's steps of it are fp32 numbers; log2(e) / T
+  __device__ __forceinline__ explicit Scale(float temperature) : t(fminf(fmaxf(temperature, 1e-36f), 1e30f)), c(1.44269504f / t) {}
 };
 // w >= min_p as a bound on x, rounded up to the next fp32.
 __device__ __forceinline__ float min_p_bound(float m, float min_p, float t) {

@@ -90,3 +90,20 @@ def test_rows_decided_in_64_bits_repeat(api):
     torch.cuda.synchronize()
     for o in outs[1:]:
         assert all(torch.equal(a, b) for a, b in zip(o, outs[0]))
+
+
+@pytest.mark.parametrize("R", [5, 640])
+def test_logits_and_temperatures_next_to_nothing(api, R):
+    """Differences of subnormal size weigh by themselves, not by what an overflowing 1 / T leaves of them; a temperature below 1e-36 counts as that."""
+    V = 300
+    x = -torch.rand(R, V, device=DEV, generator=torch.Generator(device=DEV).manual_seed(1))
+    u = numbers(1, R, 3)
+    check(api, x * 3e-35, u, 1, R, T=[1e-35])
+    check(api, x * 3e-36, u, 1, R, T=[1e-36], p=[0.9])
+    check(api, x * 1e-38, u, 1, R, T=[1e-36], k=[200])
+    score, token = torch.empty(R, 3, device=DEV), torch.empty(R, 3, device=DEV, dtype=torch.int32)
+    tokens = []
+    for T in (1e-36, 1e-37, 1e-40):
+        api.grace_sample(x * 3e-36, u.to(DEV), score, token, 1, R, temperature=torch.tensor([T], device=DEV))
+        tokens.append(token.clone())
+    assert torch.equal(tokens[0], tokens[1]) and torch.equal(tokens[0], tokens[2])
