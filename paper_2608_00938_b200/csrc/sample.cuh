@@ -858,8 +858,8 @@ __device__ __forceinline__ void limit_and_draw(const SampleParams& p, const Row&
 }
 
 // A row without a list yet: dense, or with more allowed tokens than a list takes.  SHARED (one warp): the row lies in the list's
-// place and is narrowed there; otherwise every pass reads it.
-template <int NW, bool BF16, bool SHARED>
+// place and is narrowed there; otherwise every pass reads it.  WHOLE: there is room for all of it when no list holds what stays.
+template <int NW, bool BF16, bool SHARED, bool WHOLE>
 __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF16> row, const Team<NW>& tm, SampleShared<NW>& sh, float* vals,
                                              uint16_t* tokens, int64_t r, int n, RowLimits l) {
   constexpr int NT = NW * 32;
@@ -1092,7 +1092,7 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
     }
   }
   // no limit, or one that leaves more than a list takes: the whole row
-  if (p.V <= p.cap) {
+  if constexpr (WHOLE) {
     if (!SHARED) {
       for (int i = 0; i < iters; ++i)
         if (first + 32 * i < quads) shared[first + 32 * i] = quad(first + 32 * i);
@@ -1100,7 +1100,7 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
     tm.sync();
     const RowShared all{vals, nullptr, p.V};
     limit_and_draw<NW, BF16>(p, all, tm, sh, r, m, l, sc, Sum<NW>(0), LeftOut<BF16>{row, 0.f}, row.inf);
-  } else if constexpr (!SHARED) {
+  } else {
     limit_and_draw<NW, BF16>(p, row, tm, sh, r, m, l, sc, Sum<NW>(0), LeftOut<BF16>{row, 0.f}, row.inf);
   }
 }
@@ -1127,27 +1127,16 @@ sample_kernel(const SampleParams p) {
   const RowGlobal<BF16> row{reinterpret_cast<const char*>(p.logits) + r * p.ld * (BF16 ? 2 : 4), allow, p.V, p.vec, false};
   int n = p.V;
   if constexpr (LISTS) {
-    // the allowed tokens' places: a thread's words are neighbours, so that the list is in order
-    const int per = (words + NT - 1) / NT;
-    auto word = [&](int i) {
-      const int w = tm.tid * per + i;
-      uint64_t a = i < per && w < words ? __ldg(allow + w) : 0ull;
-      if (w == words - 1 && (p.V & 63)) a &= (1ull << (p.V & 63)) - 1ull;
-      return a;
-    };
-    const uint64_t a0 = word(0);
-    int count = __popcll(a0);
-    for (int i = 1; i < per; ++i) count += __popcll(word(i));
-    const int upto = tm.scan(count);
+    // the allowed tokens' places: a thread has a word (run_sample's rows have no more words than threads)
+    uint64_t a = tm.tid < words ? __ldg(allow + tm.tid) : 0ull;
+    if (tm.tid == words - 1 && (p.V & 63)) a &= (1ull << (p.V & 63)) - 1ull;
+    const int count = __popcll(a), upto = tm.scan(count);
     n = NW == 1 ? __shfl_sync(kFullMask, upto, 31) : tm.reduce(upto, [](int a, int b) { return max(a, b); });
     if (n <= p.tokens_cap) {
       int at = upto - count;
-      for (int i = 0; i < per; ++i) {
-        const uint64_t a = i == 0 ? a0 : word(i);
-        const int token0 = (tm.tid * per + i) * 64;
-        for (uint32_t h = (uint32_t)a; h != 0u; h &= h - 1u) tokens[at++] = (uint16_t)(token0 + __ffs((int)h) - 1);
-        for (uint32_t h = (uint32_t)(a >> 32); h != 0u; h &= h - 1u) tokens[at++] = (uint16_t)(token0 + 31 + __ffs((int)h));
-      }
+      const int token0 = tm.tid * 64;
+      for (uint32_t h = (uint32_t)a; h != 0u; h &= h - 1u) tokens[at++] = (uint16_t)(token0 + __ffs((int)h) - 1);
+      for (uint32_t h = (uint32_t)(a >> 32); h != 0u; h &= h - 1u) tokens[at++] = (uint16_t)(token0 + 31 + __ffs((int)h));
       tm.sync();
       float m = -INFINITY;
       for (int i0 = 0; i0 < n; i0 += 4 * NT) {             // four loads in flight
@@ -1192,7 +1181,7 @@ sample_kernel(const SampleParams p) {
       return;
     }
   }
-  sample_dense<NW, BF16, SHARED>(p, row, tm, sh, vals, tokens, r, n, l);
+  sample_dense<NW, BF16, SHARED, !LISTS && NW != 32>(p, row, tm, sh, vals, tokens, r, n, l);
 }
 
 template <int NW, bool BF16, bool LISTS>
@@ -1203,7 +1192,8 @@ static grace_status_t launch_sample(SampleParams p, cudaStream_t s) {
   constexpr bool kShared = NW == 1 && !LISTS;
   constexpr int kTeams = NW == 1 ? 2 : 1;
   const int row = kShared ? (p.V + 127) & ~127 : (p.V + 15) & ~15, half = p.V <= 512 ? row : (p.V / 2 + 15) & ~15;
-  p.cap = NW == 32 ? 16384 : (LISTS ? half : row);
+  p.cap = NW == 32 ? 16384 : (LISTS ? half : row);         // (V <= 2048, 8192, 16384 with 1, 4, 8 warps: sample_dense's WHOLE)
+  static_assert(kSampleMostV <= 32 * 32 * 64, "");         // 64 tokens a thread
   p.tokens_cap = NW == 32 ? 16384 : half;
   p.team_bytes = ((int)sizeof(SampleShared<NW>) + p.cap * 4 + p.tokens_cap * 2 + 15) & ~15;
   static_assert(sizeof(SampleShared<32>) + 16384 * 6 <= 227 * 1024, "");
@@ -1225,6 +1215,7 @@ static grace_status_t run_sample(const SampleParams& p, cudaStream_t s) {
   // Rows in a list's shared memory: half the tokens' room.  (With 3/8 of it 20 warps instead of 18 are on an SM, 8 % less time for short
   // lists, but top-k 1000 of 2048 goes from 517 to 670 us, its row being read again.)
   const bool lists = p.allow != nullptr;
+  // (64 tokens a thread at the most: sample_kernel's words)
   if (p.V > 16384) return lists ? launch_sample<32, BF16, true>(p, s) : launch_sample<32, BF16, false>(p, s);
   if (p.V > 8192 || (p.V > 1024 && p.R <= kSms)) return lists ? launch_sample<8, BF16, true>(p, s) : launch_sample<8, BF16, false>(p, s);
   if (p.V > 2048 || (p.V > 256 && p.R <= 4 * kSms)) return lists ? launch_sample<4, BF16, true>(p, s) : launch_sample<4, BF16, false>(p, s);
