@@ -57,7 +57,7 @@ __device__ __forceinline__ void act_gelu_tanh(float& v0, float& v1) {
 //   bf16 results, degree 8 up to a = 9       2^-16 of itself: 1 / 128 of half a bf16 step
 //   fp32 results, degree 12 up to a = 8.6    2^-20.3 up to 2, 2^-18.5 up to 5, 2^-15.7 up to 8.6
 // From there on a stays, and what is left is above -2^-54.  (1 + erff has no digits left at -5.7; erfcf has, but took 342 us for 65536 x 2048 x 512
-// e4m3 to fp32.)
+// e4m3 to fp32, which takes 172 so and took 213 with erff.)
 __device__ __forceinline__ float act_gelu_one_f32(float v) {
   const float a = fminf(fabsf(v), 8.6f);
   float q = fmaf(a, -7.3320009785771134e-11f, 4.0688297175961452e-09f);
@@ -405,11 +405,12 @@ act_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CU
 // for another.  WIDE: rows of y and of the residual start on 16 bytes; otherwise the warp moves single elements between the
 // 2 KB and memory.
 // LONG (fp32 results of more than kAPSegment k-blocks): an accumulator takes a segment, and the epilogue's warps add them up in
-// registers while the other accumulator fills.  Segments of 16 k-blocks leave 1.0e-6 of the result; of 12, 7.3e-7 for 7 to 25 % more
-// time (7003 x 2036 x 8184 with SiLU and residual 283 -> 305 us, 20000 x 1024 x 1024 43 -> 53: the accumulators change hands
-// before they are drained); with a first one of 32 while the tile in front is finished, 281 us and 2.1e-6 at K = 2048.
-// Measured, e4m3 to bf16: 65536 x 2048 x 512 89 us (eight warps in two groups that share a buffer and its barriers: 84), with GELU
-// 130, bound by the epilogue's instructions; 65536 x 512 x 2048 61 us, 2.26 PFLOP/s, 68 with a residual.
+// registers while the other accumulator fills.  Segments of 16 k-blocks leave 1.0e-6 of the result; of 12, 7e-7 for 6 to 22 % more
+// time (7003 x 2036 x 8184 with SiLU and residual 278 -> 295 us, 20000 x 1024 x 1024 47 -> 57: the accumulators change hands
+// before they are drained); without any, 232 us and 9.1e-6.
+// Measured, e4m3 to bf16, L2 flushed between calls: 65536 x 2048 x 512 84 us, with GELU 129, bound by the epilogue's instructions;
+// 65536 x 512 x 2048 61.5 us, 2.23 PFLOP/s, 68 with a residual.  (In a row of calls the power limit leaves a lower clock: 140 with GELU, 85
+// with a residual, and 324 for 7003 x 2036 x 8184.)
 // ---------------------------------------------------------------------------------------------
 constexpr int kAPStages = 5;
 constexpr int kAPStageBytes = 2 * 128 * 128;

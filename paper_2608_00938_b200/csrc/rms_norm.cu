@@ -4,7 +4,7 @@
 //   bf16: y = n;   e4m3: scale = max(max|n|, 2^-100) / 448, y = n / scale
 // One pass over memory: the row stays in registers as fp32 between the sum of squares, the largest magnitude and the stores,
 // so a call reads x, delta and gamma once and writes the stream and y once.  Bound by HBM: 65536 x 512 bf16 with delta to e4m3
-// (235 MB) 35.2 us, 6.7 TB/s; 8191 x 2048 fp32 to bf16 (201 MB) 34 us in a row of calls, 5.9 TB/s.
+// (235 MB) 37.1 us, 6.3 TB/s; 8191 x 2048 fp32 to bf16 (201 MB) 34 us in a row of calls, 5.9 TB/s.
 #include <cuda_fp8.h>
 #include "common.cuh"
 

@@ -12,8 +12,8 @@
 // fourteen.
 // No sort: the cut is found through a histogram of 256 equal steps of (max - x) / T, in counts (top-k) or in fixed-point
 // weights (top-p), whose one step that holds the cut is then resolved value by value.
-// Measured (65536 x 2048 fp32, one draw; a read at the rate of a copy takes 82 us): no limit 304 us, T = 0 142, min-p 0.02 221, top-k 50
-// 326, top-k 200 with top-p 0.95 and min-p 0.02 471; a twentieth allowed, top-p 0.9 180.  Bound by instructions and the latency of dependent ones.
+// Measured (65536 x 2048 fp32, one draw; a read at the rate of a copy takes 82 us): no limit 310 us, T = 0 143, min-p 0.02 225, top-k 50
+// 334, top-p 0.9 520, top-p 0.95 with min-p 0.05 395, top-k 200 with top-p 0.95 and min-p 0.02 501; a twentieth allowed, top-p 0.9 175.  Bound by instructions and the latency of dependent ones.
 // The answer is that of the definition in 64 bits, at the cost of 32: weights and sums are fp32, every comparison of a sum with
 // a border has a margin above the sums' worst error, and a row for which one falls inside the margin is done again with
 // e^ and sums in fp64.
@@ -936,8 +936,8 @@ __device__ __forceinline__ void sample_dense(const SampleParams& p, RowGlobal<BF
   // a step's far edge, further by what rounding can make of it
   auto edge = [&](int step) { return m - ((float)(step + 1) * 1.0001f) / (sc.c * kSampleSteps) - fabsf(m) * 0x1p-20f; };
   // top-p: the weights' histogram leaves what is kept and a step or two; the bound on light weights alone, several times that.
-  // (65536 x 2048, top-p 0.95 at T = 1.5: 1515 us by the latter, 1095 so; 0.9 of bf16 logits 641, 560; 1024 x 16384, top-p
-  // 0.9: 142, 131.  The longest rows, of which few draw and whose threads meet in the same steps: 64 x 65472, top-p 0.95: 49, 52.)
+  // (65536 x 2048, top-p 0.95 at T = 1.5: 1608 us by the latter, 915 so; 0.9 of bf16 logits 750, 591; 1024 x 16384, top-p
+  // 0.9: 159, 144; but top-p 0.9 at T = 1 511, 520, and 0.95 with min-p 0.05, the tighter one, 282, 395.  The longest rows, of which few draw and whose threads meet in the same steps: 64 x 65472, top-p 0.95: 49, 52.)
   constexpr bool kMassHist = NW <= 8;
   if (by_count) {
     clear_hist(tm, sh);
