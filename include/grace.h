@@ -537,7 +537,8 @@ grace_status_t grace_log_softmax(float* logits, int R, int V, void* stream);
  * x_out (x's type) are both given or both NULL (s = x, nothing kept); x_out may be x, with its row stride.  Otherwise
  * outputs overlap nothing.  Row r of a tensor starts at r * its row stride (elements, >= D).  The norm is that of the
  * stored stream: one call with delta gives the bits of an addition followed by a call without.
- * Statistics in fp32.  A NaN stays in its row, whose y_scale is then NaN.  1 <= D <= 16384, R <= 2^31 - 4, any alignment
+ * Statistics in fp32: a row whose sum of squares is beyond that (|s| from about 1e18 on) comes out as zeros.  A NaN stays in its row, whose y_scale
+ * is then NaN.  1 <= D <= 16384, R <= 2^31 - 4, any alignment
  * of the elements' own; rows that all start on 16 bytes (y_e4m3: 8) with D % 8 == 0 take the wide form. */
 grace_status_t grace_rms_norm(const float* x_f32, const uint16_t* x_bf16, int64_t ldx, const uint16_t* delta,
                               int64_t ld_delta, void* x_out, int64_t ldx_out, const float* gamma,
