@@ -593,7 +593,8 @@ grace_status_t grace_linear_act_e4m3(const uint8_t* x, int64_t ldx, const float*
  * out_token: what grace_beam_update takes with K = M*draws.  A row without candidates: score and logq -inf, token 0.
  * A NaN among a row's allowed logits sets GRACE_DEV_NAN and leaves the row without candidates.  Logits of +inf weigh
  * 1 each and all others nothing.
- * The tokens are those of this definition in 64-bit arithmetic.  Nothing depends on the order of the GPU's threads.
+ * The tokens are those of this definition in 64-bit arithmetic; out_logq is a logarithm of fp32 sums, within 2^-17 + 2^-22 |log q| at the
+ * worst and 2^-23 as a rule.  Nothing depends on the order of the GPU's threads.
  * V <= 65536, draws <= 2^30, B*M < 2^31; a positive T counts as 1e-36 at least and 1e30 at most. */
 grace_status_t grace_sample(const float* logits_f32, const uint16_t* logits_bf16, int64_t ld, const uint64_t* allow_bits,
                             const float* row_score, const float* row_lse, const float* temperature,
